@@ -298,6 +298,31 @@ int32_t ulorl_token_loss_fwd_bwd_static(
     void *dlogits, const ulorl_launch *launch, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * The likeliest tokens of each row, beside the log-prob of a given one and the entropy: what a decoder
+ * shows of its alternatives, and what is recorded of a teacher for ulorl_distill_*.
+ * With x = z / temperature and p = softmax(x):
+ *   lse       [N]      ln sum_j e^x_j                     entropy  [N]  - sum_j p_j ln p_j, nats
+ *   logp      [N]      x[token_ids] - lse; not-a-number for an id outside [0, V).  token_ids may be NULL (logp is
+ *                      not written then and may be NULL)
+ *   top_ids   [N, K]   int32, the K largest logits in falling order; of equal logits (+0 and -0 are) the lower id first
+ *   top_logp  [N, K]   their x - lse
+ * logits, N, V and row_stride as in ulorl_token_loss_fwd, N < 2^31; 1 <= K <= 128; temperature in [1e-3, 1e3].
+ * A logit at or below -9e29, -infinity included, is MASKED: it has probability 0 and is no alternative; where
+ * fewer than K tokens are left (V < K too) the last ids are -1 and their log-probs -infinity.  A row that holds
+ * not-a-number or +infinity, or nothing but masked logits, gets not-a-number everywhere and ids of -1.
+ * Sums are exact to about 1e-7 for logits up to 1e8 temperature; beyond that a row may be reported as not finite.
+ *   workspace     ulorl_token_topk_workspace_bytes(N, V) bytes, 256-byte aligned, or NULL.  With one, few rows
+ *                 are read by several workgroups each; without, every row by one.  The same ids either way;
+ *                 sums differ by their order.  Its contents need not be preserved between calls.
+ */
+size_t ulorl_token_topk_workspace_bytes(int64_t N, int64_t V);
+
+int32_t ulorl_token_topk(
+    const void *logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t *token_ids,
+    int32_t K, float temperature, int32_t *top_ids, float *top_logp, float *logp, float *entropy, float *lse,
+    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------
  * lm_head variant: the logits are hidden . W and are never materialised.
  *
  *   hidden        [N, Hd] bf16 row-major (Hd contiguous), 16-byte aligned

@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     LAUNCH_PER_ROW, LAUNCH_DENSE_ROWS, Launch,
     UlorlError, Params, FwdResult, lib_path, load_library, version, status_string,
     token_loss_workspace_bytes, token_loss_fwd, token_loss_bwd, token_loss_fwd_bwd, token_loss_fwd_bwd_static, init, static_scratch_bytes, row_stats,
+    TopkResult, token_topk_workspace_bytes, token_topk,
     lmhead_workspace_bytes, lmhead_token_loss_fwd, lmhead_token_loss_bwd, gemm_tn_bf16,
     advantage_prep, segment_diagnostics, segment_pool_step,
 )

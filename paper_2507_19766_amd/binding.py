@@ -153,6 +153,11 @@ def load_library(build_if_missing: bool = True):
     lib.ulorl_static_scratch_bytes.argtypes = []
     lib.ulorl_token_loss_fwd_bwd_static.restype = c.c_int32
     lib.ulorl_token_loss_fwd_bwd_static.argtypes = lib.ulorl_token_loss_fwd_bwd.argtypes[:-4] + [vp, vp]
+    lib.ulorl_token_topk_workspace_bytes.restype = c.c_size_t
+    lib.ulorl_token_topk_workspace_bytes.argtypes = [c.c_int64, c.c_int64]
+    lib.ulorl_token_topk.restype = c.c_int32
+    lib.ulorl_token_topk.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int64, vp, c.c_int32, c.c_float,
+                                     vp, vp, vp, vp, vp, vp, c.c_size_t, vp]
     lib.ulorl_lmhead_workspace_bytes.restype = c.c_size_t
     lib.ulorl_lmhead_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int64, c.c_int32, c.c_int32]
     lib.ulorl_lmhead_token_loss_fwd.restype = c.c_int32
@@ -326,6 +331,32 @@ def token_loss_bwd(logits, token_ids, lse, gcoef, grad_out: float = 1.0,
                    dlogits: Optional[torch.Tensor] = None, inplace: bool = False) -> torch.Tensor:
     """ulorl_token_loss_bwd.  ``inplace=True`` overwrites ``logits`` with the gradient."""
     return native().token_loss_bwd(logits, token_ids, lse, gcoef, float(grad_out), dlogits, bool(inplace))
+
+
+# ------------------------------------------------------------------------------------ likeliest tokens
+
+@dataclass
+class TopkResult:
+    """Of each row: the k likeliest tokens in falling order and their log-probs [N, k], the given token's log-prob (None
+    without one), entropy and log-sum-exp [N]."""
+    top_ids: torch.Tensor
+    top_logp: torch.Tensor
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+
+
+def token_topk_workspace_bytes(N: int, V: int) -> int:
+    return int(load_library().ulorl_token_topk_workspace_bytes(N, V))
+
+
+def token_topk(logits, k: int, token_ids=None, temperature: float = 1.0, out: Optional[TopkResult] = None,
+               workspace: Optional[torch.Tensor] = None) -> TopkResult:
+    """ulorl_token_topk: the ``k`` likeliest tokens of each row under ``softmax(logits / temperature)``, of equal logits the
+    lower id first; ids of -1 and log-probs of -infinity where fewer tokens are unmasked."""
+    given = None if out is None else [out.top_ids, out.top_logp, out.logp, out.entropy, out.lse]
+    fields = native().token_topk(logits, int(k), token_ids, float(temperature), given, workspace)
+    return TopkResult(*fields)
 
 
 # ------------------------------------------------------------------------------------ lm_head variant

@@ -1809,7 +1809,7 @@ int32_t fwd_bwd_enqueue(const void* logits, int32_t dt, int64_t N, int64_t V, in
 
 extern "C" {
 
-int32_t ulorl_version(void) { return 200; }
+int32_t ulorl_version(void) { return 300; }
 
 const char* ulorl_status_string(int32_t status)
 {

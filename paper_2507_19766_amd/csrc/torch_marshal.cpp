@@ -7,6 +7,7 @@
 // a small lm_head 189 us for 70, because the backward ran Python on autograd's device thread.
 #include <ATen/ATen.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/utils/pybind.h>
@@ -268,6 +269,61 @@ Tensor token_loss_bwd(const Tensor& z, const OptTensor& token_ids, const OptTens
     return d;
 }
 
+// An [N, K] tensor that a kernel reads or writes as it lies.
+void check_matrix(const Tensor& t, at::ScalarType type, int64_t n, int64_t k, const char* name, const at::Device& dev)
+{
+    TORCH_CHECK_VALUE(t.device() == dev && t.scalar_type() == type && t.dim() == 2 && t.size(0) == n && t.size(1) == k && t.is_contiguous(),
+                      name, " must be a contiguous ", type_name(type), "[", n, ", ", k, "] tensor on ", dev.str());
+}
+Tensor empty_matrix(int64_t n, int64_t k, at::ScalarType type, const at::Device& dev)
+{
+    return at::empty({n, k}, at::TensorOptions().dtype(type).device(dev));
+}
+// A workspace of at least `need` bytes, the caller's or a new one.
+Tensor checked_workspace(const OptTensor& given, size_t need, const at::Device& dev)
+{
+    if (given.has_value())
+        TORCH_CHECK_VALUE(given->device() == dev && given->is_contiguous(), "workspace must be a contiguous tensor on ", dev.str());
+    return workspace_or(given, need, dev);
+}
+
+// The fields of TopkResult, in its order; a caller's are written or refused.
+enum { TOP_IDS, TOP_LOGP, TOP_TOKEN_LOGP, TOP_ENTROPY, TOP_LSE, TOP_FIELDS };
+using TopFields = std::array<Tensor, TOP_FIELDS>;
+
+TopFields token_topk(const Tensor& z, int64_t K, const OptTensor& token_ids, double temperature, const std::optional<std::vector<OptTensor>>& out,
+                     const OptTensor& workspace)
+{
+    const Logits l = check_logits(z);
+    const c10::DeviceGuard guard(l.dev);
+    check_vector(token_ids, at::kInt, l.N, "token_ids", l.dev);
+    TORCH_CHECK_VALUE(K >= 1 && K <= 128, "k must be 1 to 128, got ", K);
+    TopFields f;
+    if (out.has_value()) {
+        for (int i = 0; i < TOP_FIELDS; ++i) {
+            if ((*out)[i].has_value()) f[i] = *(*out)[i];
+            TORCH_CHECK_VALUE(f[i].defined() || (i == TOP_TOKEN_LOGP && !token_ids.has_value()), "out lacks a tensor");
+        }
+        check_matrix(f[TOP_IDS], at::kInt, l.N, K, "out.top_ids", l.dev);
+        check_matrix(f[TOP_LOGP], at::kFloat, l.N, K, "out.top_logp", l.dev);
+        if (token_ids.has_value()) check_vector(f[TOP_TOKEN_LOGP], at::kFloat, l.N, "out.logp", l.dev);
+        check_vector(f[TOP_ENTROPY], at::kFloat, l.N, "out.entropy", l.dev);
+        check_vector(f[TOP_LSE], at::kFloat, l.N, "out.lse", l.dev);
+    } else {
+        f[TOP_IDS] = empty_matrix(l.N, K, at::kInt, l.dev);
+        f[TOP_LOGP] = empty_matrix(l.N, K, at::kFloat, l.dev);
+        if (token_ids.has_value()) f[TOP_TOKEN_LOGP] = empty(l.N, at::kFloat, l.dev);
+        f[TOP_ENTROPY] = empty(l.N, at::kFloat, l.dev);
+        f[TOP_LSE] = empty(l.N, at::kFloat, l.dev);
+    }
+    const Tensor ws = checked_workspace(workspace, ulorl_token_topk_workspace_bytes(l.N, l.V), l.dev);
+    check(ulorl_token_topk(ptr(z), l.dt, l.N, l.V, l.stride, as<int32_t>(token_ids), (int32_t)K, (float)temperature, as<int32_t>(f[TOP_IDS]),
+                           as<float>(f[TOP_LOGP]), as<float>(f[TOP_TOKEN_LOGP]), as<float>(f[TOP_ENTROPY]), as<float>(f[TOP_LSE]), ptr(ws),
+                           ws.nbytes(), stream_of(l.dev)),
+          "ulorl_token_topk");
+    return f;
+}
+
 struct Lmhead {
     int64_t N, Hd, V;
     at::Device dev;
@@ -385,7 +441,8 @@ Fields fields_of(const Given& given)
             if ((*given)[i].has_value()) f[i] = *(*given)[i];
     return f;
 }
-py::list list_of(const Fields& f)
+template <class F>
+py::list list_of(const F& f)
 {
     py::list out;
     for (const Tensor& t : f) out.append(t.defined() ? py::cast(t) : py::object(py::none()));
@@ -444,6 +501,9 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
     });
     m.def("token_loss_bwd", [](const Tensor& z, const OptTensor& y, const OptTensor& lse, const OptTensor& g, double grad_out, const OptTensor& d,
                                bool inplace) { return unlocked([&] { return token_loss_bwd(z, y, lse, g, grad_out, d, inplace); }); });
+    m.def("token_topk", [](const Tensor& z, int64_t K, const OptTensor& y, double temperature, const Given& out, const OptTensor& ws) {
+        return list_of(unlocked([&] { return token_topk(z, K, y, temperature, out, ws); }));
+    });
     m.def("lmhead_fwd", [](const Tensor& h, const Tensor& w, OptTensor y, OptTensor cu, OptTensor adv, OptTensor old, OptTensor ids,
                            uintptr_t params, uintptr_t launch, int64_t chunk, const Given& out, const OptTensor& ws, int64_t K) {
         Fields f = fields_of(out);

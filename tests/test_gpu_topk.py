@@ -1,0 +1,253 @@
+"""token_topk against its definition in 64 bits: ids in order (ties to the lower id), log-probs, entropy, at the lengths, masks
+and ties where a selection can go wrong."""
+import math
+
+import pytest
+import torch
+
+import paper_2507_19766_amd as ulorl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 2.0 ** -23
+MASKED = -9e29
+
+
+def reference(z, k, T, y=None):
+    """Everything in 64 bits, and how far 32-bit sums may be off.  A term e^x (x <= 0, relative to the maximum) is off by the
+    rounding of its argument and one unit of the hardware's exp2, EPS (1 + |x|), and by up to eight roundings on its way
+    through the sums; the weighted sum is a chain of V / 256 fused steps per lane."""
+    z = z.double()
+    z = torch.where(z <= MASKED, -math.inf, z)
+    order = z.sort(dim=1, descending=True, stable=True)
+    m = order.values[:, :1]
+    x = (z - m) / T
+    p = torch.softmax(x, 1)
+    X = torch.where(p > 0, -x, 0.0)
+    ln_s = torch.logsumexp(x, 1)
+    eta = EPS * (10 + X)
+    mean = (p * X).sum(1, keepdim=True)
+    ref = dict(lse=(m / T)[:, 0] + ln_s, entropy=ln_s + mean[:, 0])
+    sums = (p * eta).sum(1)
+    tol = dict(lse=sums + EPS * ref["lse"].abs(),
+               entropy=(p * eta * (1 + (X - mean).abs())).sum(1) + EPS * (ref["entropy"] + (z.shape[1] / 256 + 64) * mean[:, 0]))
+    n = min(k, z.shape[1])
+    ids = torch.full((z.shape[0], k), -1, dtype=torch.int32, device=z.device)
+    logp = torch.full((z.shape[0], k), -math.inf, dtype=torch.float64, device=z.device)
+    logp[:, :n] = x.gather(1, order.indices[:, :n]) - ln_s[:, None]
+    ids[:, :n] = torch.where(logp[:, :n] > -math.inf, order.indices[:, :n], -1).int()
+    ref.update(top_ids=ids, top_logp=logp)
+    tol["top_logp"] = sums[:, None] + EPS * torch.where(logp > -math.inf, logp.abs(), 0.0)
+    if y is not None:
+        ref["logp"] = x.gather(1, y.long()[:, None])[:, 0] - ln_s
+        tol["logp"] = sums + EPS * torch.where(ref["logp"] > -math.inf, ref["logp"].abs(), 0.0)
+    return ref, tol
+
+
+def check(z, k, T=1.0, y=None, **more):
+    r = ulorl.token_topk(z, k, y, temperature=T, **more)
+    ref, tol = reference(z, k, T, y)
+    wrong = (r.top_ids != ref["top_ids"]).any(1).nonzero()[:, 0]
+    assert not len(wrong), (wrong[:5].tolist(), r.top_ids[wrong[0]].tolist()[:10], ref["top_ids"][wrong[0]].tolist()[:10])
+    for name, t in tol.items():
+        got, want = getattr(r, name).double(), ref[name]
+        fine = torch.isfinite(want)
+        assert torch.equal(got[~fine], want[~fine]), name
+        off = (got - want).abs()[fine] / t[fine]
+        assert not off.numel() or off.max() <= 1, (name, float(off.max()))
+    return r
+
+
+def rows(n, V, dtype, seed=0, pad=None, std=3.0):
+    vec = 8 if dtype == torch.bfloat16 else 4
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    z = torch.zeros(n, V + (-V % vec if pad is None else pad), dtype=dtype, device=DEV)[:, :V]
+    z.copy_(torch.randn(n, V, generator=g, device=DEV) * std)
+    return z
+
+
+def tokens(n, V, seed=0):
+    return torch.randint(0, V, (n,), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV, dtype=torch.int32)
+
+
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 63, 64, 65, 511, 2047, 2048, 2049, 4096, 10239, 10241, 20479, 20480, 20481, 32003, 40961])
+def test_lengths_of_rows(V, dtype):
+    for n, k, T in [(3, 1, 1.0), (2, 8, 0.7), (1, 33, 1.0), (5, 128, 2.0)]:
+        check(rows(n, V, dtype, V + n), k, T, tokens(n, V, V))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n,V", [(1, 151936), (37, 151936), (300, 50257), (2, 327680), (2, 327689), (1, 1 << 20), (1, (1 << 21) + 3)])
+def test_long_rows(n, V, dtype):
+    for k in (1, 20, 128):
+        check(rows(n, V, dtype, k), k, 1.0, tokens(n, V))
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 255, 256, 257, 1023, 2049])
+def test_numbers_of_rows(n):
+    check(rows(n, 32003, BF, n), 33, 1.0, tokens(n, 32003))
+    check(rows(n, 5000, F, n), 16, 1.0, tokens(n, 5000))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [100, 4096, 32003, 151936])
+@pytest.mark.parametrize("k", [1, 7, 128])
+def test_equal_logits_go_to_the_lower_id(V, k, dtype):
+    z = rows(12, V, dtype, k)
+    z[0] = 1.5                                                  # one value only
+    z[1] = -2.0
+    z[2] = 0.0
+    z[2, ::3] = -0.0                                            # equal to +0
+    z[3] = (z[3] * 0.4).round()                                 # a handful of values
+    z[4] = (torch.arange(V, device=DEV) % 5).to(dtype)          # each one spread over the row
+    z[5] = 3.0
+    z[5, V // 2] = 4.0
+    z[6] = -(torch.arange(V, device=DEV) // max(1, V // 3)).to(dtype)
+    z[7] = z[7].abs().neg()                                     # all negative, 0 nowhere
+    z[8, V // 3:V // 3 + 64] = 20.0                             # ties within one neighbourhood
+    z[9, -1] = z[9, 0] = 30.0
+    check(z, k, 1.0, tokens(12, V))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_the_largest_side_by_side_or_in_order(dtype):
+    V = 151936
+    z = rows(6, V, dtype, 5)
+    z[0, 70000:70000 + 128] = torch.linspace(20, 40, 128, device=DEV).to(dtype)         # in two neighbourhoods of 64
+    z[1] = torch.linspace(-30, 30, V, device=DEV).to(dtype)
+    z[2] = torch.linspace(30, -30, V, device=DEV).to(dtype)
+    z[3, ::64] = torch.linspace(10, 50, len(z[3, ::64]), device=DEV).to(dtype)          # one in each
+    z[4, :2048] += 40.0
+    z[5, -2048:] += 40.0
+    for k in (1, 64, 128):
+        check(z, k, 1.0, tokens(6, V))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("mask", [-math.inf, "lowest", -1e30, -3e32])
+def test_masked_logits(mask, dtype):
+    value = torch.finfo(dtype).min if mask == "lowest" else mask
+    V = 32003
+    z = rows(9, V, dtype, 3)
+    keep = torch.zeros(9, V, dtype=torch.bool, device=DEV)
+    for r, left in enumerate([1, 2, 5, 40, 127, 128, 129, 3000, V]):
+        keep[r, torch.randperm(V, device=DEV)[:left]] = True
+    z.masked_fill_(~keep, value)
+    y = keep.float().argmax(1).int()
+    for k in (1, 5, 128):
+        check(z, k, 0.7, y)
+    outside = (~keep).float().argmax(1).int()
+    r = ulorl.token_topk(z, 5, outside)
+    assert (r.logp[:8] < -1e29).all()                           # a masked token: probability 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_peaked_rows(dtype):
+    """One logit far above all others: the log-prob of that token is the small sum of the others."""
+    z = rows(8, 151936, dtype, 11)
+    z[torch.arange(8), torch.arange(8) * 15000] = torch.tensor([15., 18., 20., 24., 30., 40., 60., 100.], device=DEV).to(dtype)
+    check(z, 20, 1.0, (torch.arange(8, device=DEV) * 15000).int())
+
+
+def test_rows_that_are_no_distribution():
+    V = 5001
+    z = rows(8, V, BF, 2)
+    z[1, 77] = math.nan
+    z[3, 4999] = math.inf
+    z[4] = -math.inf
+    z[5] = torch.finfo(BF).min
+    z[6, 5000] = math.nan                                       # behind the last whole vector
+    y = tokens(8, V)
+    y[7], y[2] = V, -1
+    r = ulorl.token_topk(z, 6, y)
+    for bad in (1, 3, 4, 5, 6):
+        assert (r.top_ids[bad] == -1).all() and r.top_logp[bad].isnan().all()
+        assert r.logp[bad].isnan() and r.entropy[bad].isnan() and r.lse[bad].isnan()
+    assert r.logp[7].isnan() and r.logp[2].isnan()              # no such token
+    good = [0, 2, 7]
+    ref, _ = reference(z[good], 6, 1.0)
+    assert torch.equal(r.top_ids[good], ref["top_ids"])
+    assert (r.lse[good] - ref["lse"]).abs().max() < 1e-5
+
+
+def test_agrees_with_row_stats_and_keeps_to_its_outputs():
+    z, y = rows(65, 151936, BF, 9), tokens(65, 151936)
+    a, b = ulorl.token_topk(z, 4, y), ulorl.row_stats(z, y)
+    for name in ("lse", "logp", "entropy"):
+        assert (getattr(a, name) - getattr(b, name)).abs().max() < 2e-5
+    big = torch.full((66, 5), 7, dtype=torch.int32, device=DEV)
+    out = ulorl.TopkResult(big[:65].flatten()[:65 * 4].view(65, 4), torch.empty(65, 4, device=DEV), None, torch.empty(65, device=DEV),
+                           torch.empty(65, device=DEV))
+    r = ulorl.token_topk(z, 4, out=out)
+    assert r.logp is None and r.top_ids.data_ptr() == big.data_ptr() and torch.equal(r.top_ids, a.top_ids)
+    assert (big.flatten()[65 * 4:] == 7).all()
+
+
+@pytest.mark.parametrize("n", [1, 40, 1500])
+def test_on_a_stream_of_its_own_and_in_a_graph(n):
+    """Replays read the inputs of the moment, with other work between them; the bits are those of a call outside."""
+    z, y = rows(n, 32003, BF, 4), tokens(n, 32003)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = ulorl.token_topk(z, 12, y)
+    ws = torch.empty(max(256, ulorl.token_topk_workspace_bytes(n, 32003)), dtype=torch.uint8, device=DEV)
+    with torch.cuda.stream(side):
+        ulorl.token_topk(z, 12, y, out=out, workspace=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ulorl.token_topk(z, 12, y, out=out, workspace=ws)
+    for seed in range(4):
+        z.copy_(rows(n, 32003, BF, 20 + seed))
+        for t in (out.top_ids, out.top_logp, out.logp, out.entropy, out.lse):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = ulorl.token_topk(z, 12, y)
+        for name in ("top_ids", "top_logp", "logp", "entropy", "lse"):
+            assert torch.equal(getattr(out, name), getattr(eager, name)), name
+
+
+def test_a_lone_row_of_any_length_and_rows_that_overlap_nothing():
+    z = torch.randn(1, 32003, device=DEV)
+    check(z, 9, 1.0, tokens(1, 32003))
+    check(rows(4, 777, F, 1, pad=1000 * 4 - 777), 9, 1.0, tokens(4, 777))       # wide stride
+
+
+def test_refusals():
+    z, y = rows(4, 1000, F), tokens(4, 1000)
+    with pytest.raises(ValueError):
+        ulorl.token_topk(z, 0, y)
+    with pytest.raises(ValueError):
+        ulorl.token_topk(z, 129, y)
+    with pytest.raises(ValueError):
+        ulorl.token_topk(z, 4, y[:3])
+    with pytest.raises(ValueError):
+        ulorl.token_topk(z, 4, y.long())
+    with pytest.raises(ValueError):
+        ulorl.token_topk(z.t(), 4)
+    with pytest.raises(TypeError):
+        ulorl.token_topk(z.half(), 4)
+    for T in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(ulorl.UlorlError) as e:
+            ulorl.token_topk(z, 4, y, temperature=T)
+        assert e.value.status == -5
+    with pytest.raises(ulorl.UlorlError) as e:
+        ulorl.token_topk(torch.zeros(4, 1001, device=DEV), 4)           # rows no multiple of 16 bytes apart
+    assert e.value.status == -4
+    with pytest.raises(ulorl.UlorlError) as e:
+        ulorl.token_topk(z[:1].expand(4, 1000), 4)
+    assert e.value.status == -2
+    with pytest.raises(ulorl.UlorlError) as e:
+        ulorl.token_topk(z, 4, y, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+    assert e.value.status == -6
+    good = ulorl.token_topk(z, 4, y)
+    for name, t in [("top_ids", good.top_ids[:, :3]), ("top_logp", good.top_logp.double()), ("logp", good.logp[:3]), ("entropy", None)]:
+        bad = ulorl.TopkResult(good.top_ids, good.top_logp, good.logp, good.entropy, good.lse)
+        setattr(bad, name, t)
+        with pytest.raises(ValueError):
+            ulorl.token_topk(z, 4, y, out=bad)
