@@ -21,6 +21,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "logits_stream.hpp"
 #include "ulorl.h"
 #include "ulorl_internal.hpp"
@@ -109,13 +111,18 @@ __device__ __forceinline__ void absorb_vectors(const u32x4 (&v)[U], float scale,
     }
     const Lane before = a;
     absorb_scaled<U * E>(f, cm, scale, a);
-    // -infinity (and what the scale takes there) makes 0 * infinity of a term of T: once more with such logits at kEmpty, whose
-    // terms are 0.  NaN and +infinity stay what they are.
+    // -infinity (and what the scale takes there) makes 0 * infinity of a term of T: once more, vector by vector, with such logits at
+    // kEmpty, whose terms are 0.  NaN and +infinity stay what they are.
     if (__any(a.T != a.T)) {
         a = before;
 #pragma unroll
-        for (int k = 0; k < U * E; ++k) f[k] = f[k] < kEmpty ? kEmpty : f[k];
-        absorb_scaled<U * E>(f, cm, scale, a);
+        for (int k = 0; k < U; ++k) {
+            float g[E];
+            Tr::unpack(v[k], g);
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] = g[e] < kEmpty ? kEmpty : g[e];
+            absorb_scaled<E>(g, fmaxf(vm[k], kFloor), scale, a);
+        }
     }
 }
 
@@ -124,18 +131,19 @@ __device__ __forceinline__ float lane_max(float x)
 {
     return fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)));
 }
-// The largest over aligned runs of 2^lg lanes (lg <= 4), in each of them.  lg is uniform.
-__device__ __forceinline__ float run_max(float x, int lg)
+// The largest over aligned runs of 2^LG lanes (LG <= 4), in each of them.
+template <int LG>
+__device__ __forceinline__ float run_max(float x)
 {
-    if (lg >= 1) x = lane_max<0xB1>(x);      // lane ^ 1
-    if (lg >= 2) x = lane_max<0x4E>(x);      // lane ^ 2
-    if (lg >= 3) x = lane_max<0x141>(x);     // 7 - lane in each 8
-    if (lg >= 4) x = lane_max<0x140>(x);     // 15 - lane in each 16
+    if constexpr (LG >= 1) x = lane_max<0xB1>(x);      // lane ^ 1
+    if constexpr (LG >= 2) x = lane_max<0x4E>(x);      // lane ^ 2
+    if constexpr (LG >= 3) x = lane_max<0x141>(x);     // 7 - lane in each 8
+    if constexpr (LG >= 4) x = lane_max<0x140>(x);     // 15 - lane in each 16
     return x;
 }
 __device__ __forceinline__ float wave_max(float x)
 {
-    x = run_max(x, 4);
+    x = run_max<4>(x);
     const int i = __float_as_int(x);
     return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
                  fmaxf(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
@@ -157,7 +165,7 @@ __device__ __forceinline__ uint64_t ranked(uint32_t key, uint32_t id) { return k
 
 struct Shared {
     float gmax[kMaxGroups];
-    uint64_t elems[kElemList];
+    alignas(16) uint64_t elems[kElemList + 8];
     uint32_t groups[kGroupList];
     double S[kTopkWaves], T[kTopkWaves];
     float m[kTopkWaves];
@@ -292,16 +300,37 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     }
     __syncthreads();
     uint32_t n_groups = sh.n_groups;
-    auto each_element = [&](const auto& f) {      // f(key, id) of every element of the listed groups, shared out over the threads
+    // f(key, id) of every element of the listed groups and of those behind the last whole vector, shared out over the threads;
+    // four loads at a time, since each one is a round trip to memory
+    const int nvec = a.V / E;
+    auto each_element = [&](const auto& f) {
         const uint64_t units = (uint64_t)n_groups << a.lg;
-        for (uint64_t u = tid; u < units; u += kTopkThreads) {
-            const int64_t i = ((int64_t)sh.groups[u >> a.lg] << a.lg) + (int64_t)(u & ((1u << a.lg) - 1u));
-            if (i * E >= a.V) continue;
-            float x[E];
-            Tr::unpack(load_vector<Tr>(rowp, a.V, (int)i), x);
+        for (uint64_t u0 = 0; u0 < units; u0 += 4 * kTopkThreads) {
+            u32x4 v[4];
+            int at[4];
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(key_of(x[e]), (uint32_t)(i * E + e));
+            for (int q = 0; q < 4; ++q) {
+                const uint64_t u = u0 + q * kTopkThreads + tid;
+                v[q] = Tr::filler();
+                at[q] = nvec;
+                if (u < units) {
+                    const int64_t i = ((int64_t)sh.groups[u >> a.lg] << a.lg) + (int64_t)(u & ((1u << a.lg) - 1u));
+                    if (i < nvec) {
+                        at[q] = (int)i;
+                        v[q] = reinterpret_cast<const u32x4*>(rowp)[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (at[q] == nvec) continue;
+                float x[E];
+                Tr::unpack(v[q], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) f(key_of(x[e]), (uint32_t)(at[q] * E + e));
+            }
         }
+        if (tid < a.V - nvec * E) f(key_of(Tr::load1(rowp + nvec * E + tid)), (uint32_t)(nvec * E + tid));
     };
     bool full = n_groups > kGroupList;
     if (!full) {
@@ -336,12 +365,17 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
         __syncthreads();
     }
     const uint32_t n = min(sh.n_elems, (uint32_t)kElemList);
+    if (tid < 8) sh.elems[n + tid] = 0ull;                 // the ranks are counted eight keys at a time
+    __syncthreads();
     int32_t* ids = a.top_ids + row * a.K;
     float* logp = a.top_logp + row * a.K;
     for (uint32_t j = tid; j < n; j += kTopkThreads) {
         const uint64_t mine = sh.elems[j];
         uint32_t rank = 0;
-        for (uint32_t i = 0; i < n; ++i) rank += sh.elems[i] > mine ? 1u : 0u;
+        for (uint32_t i = 0; i < n; i += 8) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) rank += sh.elems[i + q] > mine ? 1u : 0u;
+        }
         if (rank < K) {
             ids[rank] = (int32_t)(0xffffffffu - (uint32_t)mine);
             logp[rank] = (float)(((double)value_of((uint32_t)(mine >> 32)) - (double)st.m) * a.inv_t - ln_s);
@@ -353,8 +387,9 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     }
 }
 
-// One workgroup per row.
-template <class Tr>
+// One workgroup per row.  LG: log2 of the vectors in a group, kManyVectors: a.lg, more than a run of 16 lanes.
+constexpr int kManyVectors = 5;
+template <class Tr, int LG>
 __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
 {
     constexpr int NT = kTopkThreads, U = kTopkUnroll, E = Tr::kPerVec;
@@ -364,50 +399,60 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
     const typename Tr::elem* rowp = logits + row * a.row_stride;
     const int nvec = a.V / E, all = (a.V + E - 1) / E;
     const int ngroups = (all + (1 << a.lg) - 1) >> a.lg;
-    if (a.lg > 4) {
+    if constexpr (LG == kManyVectors) {
         for (int g = tid; g < ngroups; g += NT) sh.gmax[g] = kEmpty;
         __syncthreads();
     }
-    // a vector's maximum into its group's
-    auto note = [&](float vm, int i) {
-        const float g = run_max(vm, a.lg > 4 ? 4 : a.lg);
-        if (i >= all) return;
-        if (a.lg > 4) {
-            if ((tid & 15) == 0) atomicMax(&sh.gmax[i >> a.lg], g);
-        } else if ((tid & ((1 << a.lg) - 1)) == 0) {
-            sh.gmax[i >> a.lg] = g;
+    // a vector's maximum into its group's: every lane of a run writes the same
+    auto note = [&](float vm, int i, bool here) {
+        const float g = run_max<(LG < 4 ? LG : 4)>(vm);
+        if constexpr (LG == kManyVectors) {
+            if (here && (tid & 15) == 0) atomicMax(&sh.gmax[i >> a.lg], g);
+        } else if (here) {
+            sh.gmax[i >> LG] = g;
         }
     };
+    const int32_t y = a.token_ids ? a.token_ids[row] : -1;
+    const bool has_y = y >= 0 && y < a.V;
+    const float zy = has_y ? Tr::load1(rowp + y) : 0.0f;      // ahead of the stream, so that nothing waits for it at the end
     Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
+    auto batch = [&](const auto& v, int first, auto whole) {
+        constexpr int B = sizeof(v) / sizeof(u32x4);
+        float vm[B];
+        absorb_vectors<Tr, B>(v, a.scale, acc, vm);
+#pragma unroll
+        for (int k = 0; k < B; ++k) note(vm[k], first + k * NT + tid, whole || first + k * NT + tid < all);
+    };
     int base = 0;
     for (; base + U * NT <= nvec; base += U * NT) {
         u32x4 v[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) v[k] = load_stream(reinterpret_cast<const u32x4*>(rowp) + base + k * NT + tid);
-        float vm[U];
-        absorb_vectors<Tr, U>(v, a.scale, acc, vm);
 #pragma unroll
-        for (int k = 0; k < U; ++k) note(vm[k], base + k * NT + tid);
+        for (int k = 0; k < U; k += 4) {
+            const u32x4 four[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
+            batch(four, base + k * NT, std::true_type{});
+        }
     }
-    for (; base < all; base += NT) {
-        const u32x4 v[1] = {load_vector<Tr>(rowp, a.V, base + tid)};
-        float vm[1];
-        absorb_vectors<Tr, 1>(v, a.scale, acc, vm);
-        note(vm[0], base + tid);
+    if (base < all) {       // the rest, its loads together, what there is of it two vectors at a time
+        u32x4 v[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) v[k] = load_vector<Tr>(rowp, a.V, base + k * NT + tid);
+#pragma unroll
+        for (int k = 0; k < U; k += 2) {
+            if (base + k * NT >= all) break;
+            const u32x4 two[2] = {v[k], v[k + 1]};
+            batch(two, base + k * NT, std::false_type{});
+        }
     }
     const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
     const double ln_s = log(st.S);
     const bool ok = st.m > kFloor && st.S >= 0.5 && st.S < 1.0e30;       // neither NaN, +infinity nor everything masked
     if (tid == 0) {
-        const int32_t y = a.token_ids ? a.token_ids[row] : -1;
         const float nan = __builtin_nanf("");
         a.lse[row] = ok ? (float)((double)st.m * a.inv_t + ln_s) : nan;
         a.entropy[row] = ok ? (float)(ln_s - st.T * (double)kLn2 / st.S) : nan;
-        if (a.logp) {
-            float lp = nan;
-            if (ok && y >= 0 && y < a.V) lp = (float)(((double)Tr::load1(rowp + y) - (double)st.m) * a.inv_t - ln_s);
-            a.logp[row] = lp;
-        }
+        if (a.logp) a.logp[row] = ok && has_y ? (float)(((double)zy - (double)st.m) * a.inv_t - ln_s) : nan;
     }
     if (!ok) {
         for (int j = tid; j < a.K; j += NT) {
@@ -417,6 +462,23 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
         return;
     }
     select_and_write<Tr>(a, rowp, row, ngroups, st, ln_s, sh);
+}
+
+template <class Tr>
+void launch_topk_rows(const void* logits, const TopkArgs& a, hipStream_t st)
+{
+    auto go = [&](auto lg) {
+        constexpr int LG = decltype(lg)::value;
+        hipLaunchKernelGGL((topk_row_kernel<Tr, LG>), dim3((unsigned)a.N), dim3(kTopkThreads), 0, st, (const typename Tr::elem*)logits, a);
+    };
+    switch (a.lg) {
+    case 0: return go(std::integral_constant<int, 0>{});
+    case 1: return go(std::integral_constant<int, 1>{});
+    case 2: return go(std::integral_constant<int, 2>{});
+    case 3: return go(std::integral_constant<int, 3>{});
+    case 4: return go(std::integral_constant<int, 4>{});
+    default: return go(std::integral_constant<int, kManyVectors>{});
+    }
 }
 
 }  // namespace
@@ -451,9 +513,9 @@ int32_t ulorl_token_topk(const void* logits, int32_t dt, int64_t N, int64_t V, i
     while (((all + ((int64_t)1 << a.lg) - 1) >> a.lg) > kMaxGroups) ++a.lg;
     hipStream_t st = (hipStream_t)hip_stream;
     if (dt == ULORL_BF16)
-        hipLaunchKernelGGL((topk_row_kernel<StoreBF16>), dim3((unsigned)N), dim3(kTopkThreads), 0, st, (const uint16_t*)logits, a);
+        launch_topk_rows<StoreBF16>(logits, a, st);
     else
-        hipLaunchKernelGGL((topk_row_kernel<StoreF32>), dim3((unsigned)N), dim3(kTopkThreads), 0, st, (const float*)logits, a);
+        launch_topk_rows<StoreF32>(logits, a, st);
     return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
 }
 
