@@ -64,24 +64,39 @@ struct Lane {
     float m, mL, S, Sc, T;
 };
 
+// The larger, not-a-number if one is (a row that holds one is refused at its end): one instruction for three values, and none to
+// quiet what came out of bit operations, which fmaxf needs.
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
 template <int COUNT>
 __device__ __forceinline__ void absorb_scaled(const float* f, float cm, float scale, Lane& a)
 {
-    const float mn = fmaxf(a.m, cm);
+    const float mn = larger(a.m, cm);
     const float mLn = mn * scale;
     const float d = a.mL - mLn;
     const float sc = fast_exp2(d);
     float T = sc * fmaf(d, a.S, a.T);
     const float S = sc * a.S, Sc = sc * a.Sc;
-    float e[COUNT];
+    // the terms as a tree over neighbours: a sum of eight is done before the next eight terms are formed
+    float e[COUNT / 8 > 0 ? COUNT / 8 : 1];
 #pragma unroll
-    for (int k = 0; k < COUNT; ++k) {
-        const float x = fmaf(f[k], scale, -mLn);
-        e[k] = fast_exp2(x);
-        T = fmaf(e[k], x, T);
+    for (int c = 0; c < COUNT; c += 8) {
+        constexpr int W = COUNT < 8 ? COUNT : 8;
+        float p[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const float x = fmaf(f[c + k], scale, -mLn);
+            p[k] = fast_exp2(x);
+            T = fmaf(p[k], x, T);
+        }
+#pragma unroll
+        for (int w = W / 2; w >= 1; w >>= 1)
+#pragma unroll
+            for (int k = 0; k < w; ++k) p[k] += p[k + w];
+        e[c / 8] = p[0];
     }
 #pragma unroll
-    for (int w = COUNT / 2; w >= 1; w >>= 1)
+    for (int w = COUNT / 16; w >= 1; w >>= 1)
 #pragma unroll
         for (int k = 0; k < w; ++k) e[k] += e[k + w];
     const float t = S + e[0];                   // TwoSum: the residual of a small term against a sum near 1 is kept
@@ -105,9 +120,9 @@ __device__ __forceinline__ void absorb_vectors(const u32x4 (&v)[U], float scale,
         Tr::unpack(v[k], f + k * E);
         float m = f[k * E];
 #pragma unroll
-        for (int e = 1; e < E; ++e) m = fmaxf(m, f[k * E + e]);
+        for (int e = 1; e < E; ++e) m = larger(m, f[k * E + e]);
         vm[k] = m;
-        cm = fmaxf(cm, m);
+        cm = larger(cm, m);
     }
     const Lane before = a;
     absorb_scaled<U * E>(f, cm, scale, a);
@@ -117,36 +132,61 @@ __device__ __forceinline__ void absorb_vectors(const u32x4 (&v)[U], float scale,
         a = before;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
+            u32x4 again = v[k];
+            asm volatile("" : "+v"(again));      // unpacked anew, instead of every logit being kept until here
             float g[E];
-            Tr::unpack(v[k], g);
+            Tr::unpack(again, g);
 #pragma unroll
             for (int e = 0; e < E; ++e) g[e] = g[e] < kEmpty ? kEmpty : g[e];
-            absorb_scaled<E>(g, fmaxf(vm[k], kFloor), scale, a);
+            absorb_scaled<E>(g, larger(vm[k], kFloor), scale, a);
         }
     }
 }
 
 template <int CTRL>
-__device__ __forceinline__ float lane_max(float x)
+__device__ __forceinline__ float from_lane(float x)
 {
-    return fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)));
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
 }
-// The largest over aligned runs of 2^LG lanes (LG <= 4), in each of them.
-template <int LG>
-__device__ __forceinline__ float run_max(float x)
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140, kRotate8 = 0x128;      // 7 - lane in each 8, 15 - lane in each 16
+// Of two vectors' maxima a lane keeps the one that its bit says, with what its partner has of it.
+template <int CTRL>
+__device__ __forceinline__ float keep_one(float lo, float hi, bool bit)
 {
-    if constexpr (LG >= 1) x = lane_max<0xB1>(x);      // lane ^ 1
-    if constexpr (LG >= 2) x = lane_max<0x4E>(x);      // lane ^ 2
-    if constexpr (LG >= 3) x = lane_max<0x141>(x);     // 7 - lane in each 8
-    if constexpr (LG >= 4) x = lane_max<0x140>(x);     // 15 - lane in each 16
-    return x;
+    const float keep = bit ? hi : lo, send = bit ? lo : hi;
+    return larger(keep, from_lane<CTRL>(send));
+}
+// Of four vectors' maxima per lane, over aligned runs of 2^LG lanes: the one that kept_vector says.  (Halving the values with each
+// step takes 14 instructions where reducing each vector takes 24.)
+template <int LG>
+__device__ __forceinline__ float run_max4(const float (&vm)[4], int lane)
+{
+    static_assert(LG >= 2 && LG <= 4, "runs of 4, 8 or 16 lanes");
+    if constexpr (LG == 2) {
+        const bool b1 = (lane & 2) != 0, b0 = (lane & 1) != 0;
+        return keep_one<kXor1>(keep_one<kXor2>(vm[0], vm[2], b1), keep_one<kXor2>(vm[1], vm[3], b1), b0);
+    } else {
+        const bool b2 = (lane & 4) != 0, b1 = (lane & 2) != 0;
+        float x = keep_one<kXor2>(keep_one<kMirror8>(vm[0], vm[2], b2), keep_one<kMirror8>(vm[1], vm[3], b2), b1);
+        x = larger(x, from_lane<kXor1>(x));
+        if constexpr (LG == 4) x = larger(x, from_lane<kRotate8>(x));
+        return x;
+    }
+}
+template <int LG>
+__device__ __forceinline__ int kept_vector(int lane)
+{
+    return LG == 2 ? (lane & 3) : ((lane >> 1) & 3);
 }
 __device__ __forceinline__ float wave_max(float x)
 {
-    x = run_max<4>(x);
+    x = larger(x, from_lane<kXor1>(x));
+    x = larger(x, from_lane<kXor2>(x));
+    x = larger(x, from_lane<kMirror8>(x));
+    x = larger(x, from_lane<kMirror16>(x));
     const int i = __float_as_int(x);
-    return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
-                 fmaxf(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
+    return larger(larger(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
+                  larger(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
 }
 
 // Order-preserving bits of a logit, -0 as +0; 0: masked.
@@ -160,6 +200,7 @@ __device__ __forceinline__ float value_of(uint32_t key)
 {
     return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
+__device__ __forceinline__ uint32_t key_of_floor() { return ~__float_as_uint(kFloor); }
 // Of equal logits the lower id is the larger key; 0: masked.
 __device__ __forceinline__ uint64_t ranked(uint32_t key, uint32_t id) { return key == 0u ? 0ull : ((uint64_t)key << 32) | (0xffffffffu - id); }
 
@@ -172,6 +213,7 @@ struct Shared {
     uint32_t bound[kTopkWaves];
     uint32_t counts[2][kTopkWaves];
     uint32_t n_groups, n_elems;
+    double ln_s;                    // ln of the row's sum, by thread 0
 };
 
 // The statistics of a row, from the lanes': largest logit, sum and weighted sum (log2 units), in every thread.
@@ -266,7 +308,7 @@ __device__ uint64_t kth_ranked(const Each& each, uint32_t K, Shared& sh)
 // The K largest of a row whose groups' maxima are in sh.gmax, written in order.  All threads of the workgroup call it after a
 // barrier; row is the same in all of them.
 template <class Tr>
-__device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, double ln_s, Shared& sh)
+__device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, Shared& sh)
 {
     constexpr int E = Tr::kPerVec;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -274,13 +316,20 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     const uint32_t per_wave = (K + kTopkWaves - 1) / kTopkWaves;
 
     // lower bound of the K-th largest; neighbouring groups go to different waves, so that each wave has its share of a short row
-    auto group_at = [&](int i) { return (i * 64 + lane) * kTopkWaves + wave; };
-    uint32_t best = 0;
-    for (int i = 0; group_at(i) < ngroups; ++i) best = max(best, key_of(sh.gmax[group_at(i)]));
+    constexpr int kPerLane = kMaxGroups / kTopkThreads;
+    float mine[kPerLane];
+    float best = kFloor;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        const int g = (i * 64 + lane) * kTopkWaves + wave;
+        mine[i] = g < ngroups ? sh.gmax[g] : kFloor;
+        best = fmaxf(best, mine[i]);
+    }
+    const uint32_t best_key = key_of(best);
     uint32_t t = 0;
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t c = t | (1u << bit);
-        const uint32_t n = (uint32_t)__popcll(__ballot(best >= c));
+        const uint32_t n = (uint32_t)__popcll(__ballot(best_key >= c));
         if (n >= per_wave) t = c;
         if (n == per_wave) break;
     }
@@ -289,18 +338,18 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTopkWaves; ++w) t = min(t, sh.bound[w]);
-    t = max(t, 1u);
+    const float bound = value_of(max(t, key_of_floor() + 1u));
 
-    for (int i = 0; group_at(i) < ngroups; ++i) {
-        const int g = group_at(i);
-        if (key_of(sh.gmax[g]) >= t) {
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        if (mine[i] >= bound) {
             const uint32_t at = atomicAdd(&sh.n_groups, 1u);
-            if (at < kGroupList) sh.groups[at] = (uint32_t)g;
+            if (at < kGroupList) sh.groups[at] = (uint32_t)((i * 64 + lane) * kTopkWaves + wave);
         }
     }
     __syncthreads();
     uint32_t n_groups = sh.n_groups;
-    // f(key, id) of every element of the listed groups and of those behind the last whole vector, shared out over the threads;
+    // f(logit, id) of every element of the listed groups and of those behind the last whole vector, shared out over the threads;
     // four loads at a time, since each one is a round trip to memory
     const int nvec = a.V / E;
     auto each_element = [&](const auto& f) {
@@ -327,17 +376,17 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
                 float x[E];
                 Tr::unpack(v[q], x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) f(key_of(x[e]), (uint32_t)(at[q] * E + e));
+                for (int e = 0; e < E; ++e) f(x[e], (uint32_t)(at[q] * E + e));
             }
         }
-        if (tid < a.V - nvec * E) f(key_of(Tr::load1(rowp + nvec * E + tid)), (uint32_t)(nvec * E + tid));
+        if (tid < a.V - nvec * E) f(Tr::load1(rowp + nvec * E + tid), (uint32_t)(nvec * E + tid));
     };
     bool full = n_groups > kGroupList;
     if (!full) {
-        each_element([&](uint32_t key, uint32_t id) {
-            if (key >= t) {
+        each_element([&](float x, uint32_t id) {
+            if (x >= bound) {
                 const uint32_t at = atomicAdd(&sh.n_elems, 1u);
-                if (at < kElemList) sh.elems[at] = ranked(key, id);
+                if (at < kElemList) sh.elems[at] = ranked(key_of(x), id);
             }
         });
         __syncthreads();
@@ -355,9 +404,9 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
         }
         __syncthreads();
         n_groups = sh.n_groups;
-        const uint64_t te = kth_ranked([&](const auto& f) { each_element([&](uint32_t key, uint32_t id) { f(ranked(key, id)); }); }, K, sh);
-        each_element([&](uint32_t key, uint32_t id) {
-            const uint64_t r = ranked(key, id);
+        const uint64_t te = kth_ranked([&](const auto& f) { each_element([&](float x, uint32_t id) { f(ranked(key_of(x), id)); }); }, K, sh);
+        each_element([&](float x, uint32_t id) {
+            const uint64_t r = ranked(key_of(x), id);
             if (r == 0ull || r < te) return;
             const uint32_t at = atomicAdd(&sh.n_elems, 1u);
             if (at < kElemList) sh.elems[at] = r;
@@ -367,6 +416,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     const uint32_t n = min(sh.n_elems, (uint32_t)kElemList);
     if (tid < 8) sh.elems[n + tid] = 0ull;                 // the ranks are counted eight keys at a time
     __syncthreads();
+    const double ln_s = sh.ln_s;
     int32_t* ids = a.top_ids + row * a.K;
     float* logp = a.top_logp + row * a.K;
     for (uint32_t j = tid; j < n; j += kTopkThreads) {
@@ -403,52 +453,57 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
         for (int g = tid; g < ngroups; g += NT) sh.gmax[g] = kEmpty;
         __syncthreads();
     }
-    // a vector's maximum into its group's: every lane of a run writes the same
-    auto note = [&](float vm, int i, bool here) {
-        const float g = run_max<(LG < 4 ? LG : 4)>(vm);
-        if constexpr (LG == kManyVectors) {
-            if (here && (tid & 15) == 0) atomicMax(&sh.gmax[i >> a.lg], g);
-        } else if (here) {
-            sh.gmax[i >> LG] = g;
+    // the largest of each of this thread's four vectors, 256 apart from `first` on, into their groups'
+    auto note = [&](const float (&vm)[4], int first, auto whole) {
+        if constexpr (LG < 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float g = vm[k];
+                if constexpr (LG == 1) g = larger(g, from_lane<kXor1>(g));
+                if (whole || first + k * NT + tid < all) sh.gmax[(first >> LG) + k * (NT >> LG) + (tid >> LG)] = g;
+            }
+        } else {
+            constexpr int RUN = LG < 4 ? LG : 4;
+            const float g = run_max4<RUN>(vm, tid);
+            const int k = kept_vector<RUN>(tid), at = k * NT + (tid & -(1 << RUN));      // from first on
+            if (whole || first + at < all) {
+                if constexpr (LG == kManyVectors) atomicMax(&sh.gmax[(first + at) >> a.lg], g);
+                else sh.gmax[(first >> LG) + (at >> LG)] = g;
+            }
         }
     };
     const int32_t y = a.token_ids ? a.token_ids[row] : -1;
     const bool has_y = y >= 0 && y < a.V;
     const float zy = has_y ? Tr::load1(rowp + y) : 0.0f;      // ahead of the stream, so that nothing waits for it at the end
     Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
-    auto batch = [&](const auto& v, int first, auto whole) {
-        constexpr int B = sizeof(v) / sizeof(u32x4);
-        float vm[B];
-        absorb_vectors<Tr, B>(v, a.scale, acc, vm);
-#pragma unroll
-        for (int k = 0; k < B; ++k) note(vm[k], first + k * NT + tid, whole || first + k * NT + tid < all);
+    auto take = [&](const u32x4* v, int first, auto whole) {
+        const u32x4 four[4] = {v[0], v[1], v[2], v[3]};
+        float vm[4];
+        absorb_vectors<Tr, 4>(four, a.scale, acc, vm);
+        note(vm, first, whole);
     };
     int base = 0;
     for (; base + U * NT <= nvec; base += U * NT) {
         u32x4 v[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) v[k] = load_stream(reinterpret_cast<const u32x4*>(rowp) + base + k * NT + tid);
+        for (int k = 0; k < U; ++k)      // uniform base, lane offset
+            v[k] = load_stream(reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(rowp) + ((size_t)(base + k * NT) << 4) + ((uint32_t)tid << 4)));
 #pragma unroll
-        for (int k = 0; k < U; k += 4) {
-            const u32x4 four[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
-            batch(four, base + k * NT, std::true_type{});
-        }
+        for (int k = 0; k < U; k += 4) take(v + k, base + k * NT, std::true_type{});
     }
-    if (base < all) {       // the rest, its loads together, what there is of it two vectors at a time
+    if (base < all) {       // the rest, its loads together
         u32x4 v[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) v[k] = load_vector<Tr>(rowp, a.V, base + k * NT + tid);
 #pragma unroll
-        for (int k = 0; k < U; k += 2) {
-            if (base + k * NT >= all) break;
-            const u32x4 two[2] = {v[k], v[k + 1]};
-            batch(two, base + k * NT, std::false_type{});
-        }
+        for (int k = 0; k < U; k += 4)
+            if (base + k * NT < all) take(v + k, base + k * NT, std::false_type{});
     }
     const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
-    const double ln_s = log(st.S);
     const bool ok = st.m > kFloor && st.S >= 0.5 && st.S < 1.0e30;       // neither NaN, +infinity nor everything masked
     if (tid == 0) {
+        const double ln_s = log(st.S);
+        sh.ln_s = ln_s;
         const float nan = __builtin_nanf("");
         a.lse[row] = ok ? (float)((double)st.m * a.inv_t + ln_s) : nan;
         a.entropy[row] = ok ? (float)(ln_s - st.T * (double)kLn2 / st.S) : nan;
@@ -461,7 +516,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
         }
         return;
     }
-    select_and_write<Tr>(a, rowp, row, ngroups, st, ln_s, sh);
+    select_and_write<Tr>(a, rowp, row, ngroups, st, sh);
 }
 
 template <class Tr>
