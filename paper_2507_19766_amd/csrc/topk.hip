@@ -488,6 +488,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
 #pragma unroll
         for (int k = 0; k < U; ++k)      // uniform base, lane offset
             v[k] = load_stream(reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(rowp) + ((size_t)(base + k * NT) << 4) + ((uint32_t)tid << 4)));
+        __builtin_amdgcn_sched_barrier(0);      // all of them on their way before the first is used
 #pragma unroll
         for (int k = 0; k < U; k += 4) take(v + k, base + k * NT, std::true_type{});
     }
