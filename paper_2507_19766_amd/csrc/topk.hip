@@ -9,7 +9,7 @@
 //      permutations more.  The groups' maxima stay in LDS (at most kMaxGroups).
 //   2. A lower bound t of the K-th largest element: each wave finds the ceil(K / waves)-th largest of its lanes' largest
 //      group maxima by bisection over ballots; t is the smallest of the waves' values, so at least K groups reach t.
-//   3. Only groups that reach t (about 1.5 K of 2374) are read again, and their elements that reach t are collected: about as
+//   3. Only groups that reach t (about 1.5 K of 2374) are read again, and their elements that reach t are listed: about as
 //      many.  Each one's rank among them is its place in the answer.
 //
 // Ties: the order is by logit and then by the lower id, as one 64-bit key per element, so every rank is taken once.
@@ -38,8 +38,17 @@ constexpr int kTopkWaves = kTopkThreads / 64;
 constexpr int kTopkUnroll = 8;
 constexpr int kMaxK = 128;
 constexpr int kMaxGroups = 2560;      // group maxima of a row: 10 KB of LDS
-constexpr int kGroupList = 512;
-constexpr int kElemList = 768;
+constexpr int kGroupsPerWave = 128;   // of the lists that a wave makes
+constexpr int kElemsPerWave = 192;
+constexpr int kElemSlots = kElemsPerWave + 8;
+constexpr uint32_t kOverflow = 0xffffffffu;
+static_assert(kMaxK <= kElemsPerWave && kMaxK <= kGroupsPerWave, "where a list overflows, K groups and K elements take its place");
+// Where rows are split: few of them, each long.  us, split / one workgroup a row: 1 row of 151936 bf16 12 / 16, fp32 12 / 25; 128 rows 20 / 23 and
+// 24 / 29; 256 rows 26 / 24 and 36 / 32; 1 row of 32000 bf16 11.5 / 9.1.
+constexpr int kMaxPieces = 64;
+constexpr int64_t kSplitRows = 160;
+constexpr int64_t kSplitBatches = 8;          // of 16 KB
+constexpr int64_t kFewWorkgroups = 1024;
 // Logits at or below -9e29 are masked (the filler of short vectors is one of them).  A lane's running maximum starts a little
 // above: by so much that the terms of masked logits are 0 against it (the rounding of m scale is 1e23 there).
 constexpr float kFloor = -8.99e29f;
@@ -54,6 +63,7 @@ struct TopkArgs {
     int64_t N, row_stride;
     int32_t V, K;
     int32_t lg;                 // log2 of the vectors in a group
+    int32_t piece_vectors;      // vectors of a piece, where a row is split
     float scale;                // log2(e) / T
     double inv_t;
 };
@@ -206,13 +216,13 @@ __device__ __forceinline__ uint64_t ranked(uint32_t key, uint32_t id) { return k
 
 struct Shared {
     float gmax[kMaxGroups];
-    alignas(16) uint64_t elems[kElemList + 8];
-    uint32_t groups[kGroupList];
+    alignas(16) uint64_t elems[kTopkWaves * kElemSlots];
+    uint32_t groups[kTopkWaves * kGroupsPerWave];
     double S[kTopkWaves], T[kTopkWaves];
     float m[kTopkWaves];
     uint32_t bound[kTopkWaves];
     uint32_t counts[2][kTopkWaves];
-    uint32_t n_groups, n_elems;
+    uint32_t found[kTopkWaves];
     double ln_s;                    // ln of the row's sum, by thread 0
 };
 
@@ -305,8 +315,52 @@ __device__ uint64_t kth_ranked(const Each& each, uint32_t K, Shared& sh)
     return t;
 }
 
+// The lanes of this wave that hit, below this one.
+__device__ __forceinline__ uint32_t hits_below(uint64_t hits)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0u));
+}
+
+// f(logit, id) of every element of n listed groups, shared out over `lanes` threads of which this is number `lane`; all threads of
+// a wave call f together, one that has no element with a masked logit.  Eight loads at a time: each is a round trip to memory.
+template <class Tr, class F>
+__device__ __forceinline__ void each_element(const TopkArgs& a, const typename Tr::elem* rowp, const uint32_t* list, uint32_t n, uint32_t lane,
+                                             uint32_t lanes, const F& f)
+{
+    constexpr int E = Tr::kPerVec, B = 8;
+    const int nvec = a.V / E;
+    const uint64_t units = (uint64_t)n << a.lg;
+    for (uint64_t u0 = 0; u0 < units; u0 += B * lanes) {
+        u32x4 v[B];
+        int at[B];
+#pragma unroll
+        for (int q = 0; q < B; ++q) {
+            const uint64_t u = u0 + q * lanes + lane;
+            v[q] = Tr::filler();
+            at[q] = 0;
+            if (u < units) {
+                const int64_t i = ((int64_t)list[u >> a.lg] << a.lg) + (int64_t)(u & ((1u << a.lg) - 1u));
+                if (i < nvec) {
+                    at[q] = (int)i;
+                    v[q] = reinterpret_cast<const u32x4*>(rowp)[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < B; ++q) {
+            if (u0 + q * lanes >= units) break;
+            float x[E];
+            Tr::unpack(v[q], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(x[e], (uint32_t)(at[q] * E + e));
+        }
+    }
+}
+
 // The K largest of a row whose groups' maxima are in sh.gmax, written in order.  All threads of the workgroup call it after a
-// barrier; row is the same in all of them.
+// barrier; row is the same in all of them.  Each wave lists the groups and elements that are its own (neighbouring groups are
+// different waves'), so that two barriers are enough.  Cycles at 151936 logits, K 64, 2048 rows in flight: bound 2000, list 1000,
+// elements 4500, ranks 3000, of 85000 for the row.
 template <class Tr>
 __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, Shared& sh)
 {
@@ -314,143 +368,148 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t K = (uint32_t)a.K;
     const uint32_t per_wave = (K + kTopkWaves - 1) / kTopkWaves;
+    const int behind = (a.V / E) * E, tail = a.V - behind;       // elements behind the last whole vector
 
-    // lower bound of the K-th largest; neighbouring groups go to different waves, so that each wave has its share of a short row
+    // lower bound of the K-th largest
     constexpr int kPerLane = kMaxGroups / kTopkThreads;
+    auto group_of = [&](int i) { return (i * 64 + lane) * kTopkWaves + wave; };
     float mine[kPerLane];
     float best = kFloor;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-        const int g = (i * 64 + lane) * kTopkWaves + wave;
-        mine[i] = g < ngroups ? sh.gmax[g] : kFloor;
-        best = fmaxf(best, mine[i]);
+        mine[i] = group_of(i) < ngroups ? sh.gmax[group_of(i)] : kFloor;
+        best = larger(best, mine[i]);
     }
     const uint32_t best_key = key_of(best);
     uint32_t t = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t c = t | (1u << bit);
-        const uint32_t n = (uint32_t)__popcll(__ballot(best_key >= c));
-        if (n >= per_wave) t = c;
+    for (int bit = 30; bit >= 0; bit -= 2) {        // two bits a step: the steps are a chain of scalar instructions
+        const uint32_t c1 = t | (1u << bit), c2 = t | (2u << bit), c3 = t | (3u << bit);
+        const uint32_t n1 = (uint32_t)__popcll(__ballot(best_key >= c1)), n2 = (uint32_t)__popcll(__ballot(best_key >= c2)),
+                       n3 = (uint32_t)__popcll(__ballot(best_key >= c3));
+        const uint32_t n = n3 >= per_wave ? n3 : n2 >= per_wave ? n2 : n1;
+        t = n3 >= per_wave ? c3 : n2 >= per_wave ? c2 : n1 >= per_wave ? c1 : t;
         if (n == per_wave) break;
     }
     if (lane == 0) sh.bound[wave] = t;
-    if (tid == 0) sh.n_groups = sh.n_elems = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTopkWaves; ++w) t = min(t, sh.bound[w]);
     const float bound = value_of(max(t, key_of_floor() + 1u));
 
+    // this wave's groups that reach it, and their elements that do
+    uint32_t* groups = sh.groups + wave * kGroupsPerWave;
+    uint64_t* elems = sh.elems + wave * kElemSlots;
+    uint32_t n_groups = 0, n_elems = 0;         // uniform
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-        if (mine[i] >= bound) {
-            const uint32_t at = atomicAdd(&sh.n_groups, 1u);
-            if (at < kGroupList) sh.groups[at] = (uint32_t)((i * 64 + lane) * kTopkWaves + wave);
-        }
+        const uint64_t hits = __ballot(mine[i] >= bound);
+        const uint32_t at = n_groups + hits_below(hits);
+        if (mine[i] >= bound && at < kGroupsPerWave) groups[at] = (uint32_t)group_of(i);
+        n_groups += (uint32_t)__popcll(hits);
     }
-    __syncthreads();
-    uint32_t n_groups = sh.n_groups;
-    // f(logit, id) of every element of the listed groups and of those behind the last whole vector, shared out over the threads;
-    // four loads at a time, since each one is a round trip to memory
-    const int nvec = a.V / E;
-    auto each_element = [&](const auto& f) {
-        const uint64_t units = (uint64_t)n_groups << a.lg;
-        for (uint64_t u0 = 0; u0 < units; u0 += 4 * kTopkThreads) {
-            u32x4 v[4];
-            int at[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint64_t u = u0 + q * kTopkThreads + tid;
-                v[q] = Tr::filler();
-                at[q] = nvec;
-                if (u < units) {
-                    const int64_t i = ((int64_t)sh.groups[u >> a.lg] << a.lg) + (int64_t)(u & ((1u << a.lg) - 1u));
-                    if (i < nvec) {
-                        at[q] = (int)i;
-                        v[q] = reinterpret_cast<const u32x4*>(rowp)[i];
-                    }
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (at[q] == nvec) continue;
-                float x[E];
-                Tr::unpack(v[q], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) f(x[e], (uint32_t)(at[q] * E + e));
-            }
-        }
-        if (tid < a.V - nvec * E) f(Tr::load1(rowp + nvec * E + tid), (uint32_t)(nvec * E + tid));
+    auto collect = [&](float x, uint32_t id) {
+        const uint64_t hits = __ballot(x >= bound);
+        if (hits == 0ull) return;
+        const uint32_t at = n_elems + hits_below(hits);
+        if (x >= bound && at < kElemsPerWave) elems[at] = ranked(key_of(x), id);
+        n_elems += (uint32_t)__popcll(hits);
     };
-    bool full = n_groups > kGroupList;
-    if (!full) {
-        each_element([&](float x, uint32_t id) {
-            if (x >= bound) {
-                const uint32_t at = atomicAdd(&sh.n_elems, 1u);
-                if (at < kElemList) sh.elems[at] = ranked(key_of(x), id);
-            }
-        });
-        __syncthreads();
-        full = sh.n_elems > kElemList;
+    if (n_groups <= kGroupsPerWave) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        each_element<Tr>(a, rowp, groups, n_groups, lane, 64, collect);
+        if (wave == 0 && tail > 0) collect(lane < tail ? Tr::load1(rowp + behind + lane) : kEmpty, (uint32_t)(behind + lane));
     }
-    if (full) {     // uniform
+    const bool overflow = n_groups > kGroupsPerWave || n_elems > kElemsPerWave;
+    if (lane == 0) sh.found[wave] = overflow ? kOverflow : n_elems;
+    if (!overflow && lane < 8) elems[n_elems + lane] = 0ull;        // the ranks are counted eight keys at a time
+    __syncthreads();
+    uint32_t n[kTopkWaves];
+    bool full = false;
+#pragma unroll
+    for (int w = 0; w < kTopkWaves; ++w) {
+        n[w] = sh.found[w];
+        full = full || n[w] == kOverflow;
+    }
+    if (full) {     // uniform: the K-th largest key itself, of the groups and then of the elements of the K first groups
         const uint64_t tg = kth_ranked([&](const auto& f) {
             for (int g = tid; g < ngroups; g += kTopkThreads) f(ranked(key_of(sh.gmax[g]), (uint32_t)g));
         }, K, sh);
-        if (tid == 0) sh.n_groups = sh.n_elems = 0;
+        if (tid == 0) sh.found[0] = sh.found[1] = 0;
         __syncthreads();
         for (int g = tid; g < ngroups; g += kTopkThreads) {
             const uint64_t r = ranked(key_of(sh.gmax[g]), (uint32_t)g);
-            if (r != 0ull && r >= tg) sh.groups[atomicAdd(&sh.n_groups, 1u)] = (uint32_t)g;      // K at most: the keys differ
+            if (r != 0ull && r >= tg) sh.groups[atomicAdd(&sh.found[0], 1u)] = (uint32_t)g;      // K at most: the keys differ
         }
         __syncthreads();
-        n_groups = sh.n_groups;
-        const uint64_t te = kth_ranked([&](const auto& f) { each_element([&](float x, uint32_t id) { f(ranked(key_of(x), id)); }); }, K, sh);
-        each_element([&](float x, uint32_t id) {
-            const uint64_t r = ranked(key_of(x), id);
-            if (r == 0ull || r < te) return;
-            const uint32_t at = atomicAdd(&sh.n_elems, 1u);
-            if (at < kElemList) sh.elems[at] = r;
+        const uint32_t listed = sh.found[0];
+        auto each_key = [&](const auto& f) {
+            each_element<Tr>(a, rowp, sh.groups, listed, tid, kTopkThreads, [&](float x, uint32_t id) { f(ranked(key_of(x), id)); });
+            if (tid < tail) f(ranked(key_of(Tr::load1(rowp + behind + tid)), (uint32_t)(behind + tid)));
+        };
+        const uint64_t te = kth_ranked(each_key, K, sh);
+        each_key([&](uint64_t r) {
+            if (r != 0ull && r >= te) sh.elems[atomicAdd(&sh.found[1], 1u)] = r;                    // K at most
         });
         __syncthreads();
+        n[0] = sh.found[1];
+#pragma unroll
+        for (int w = 1; w < kTopkWaves; ++w) n[w] = 0;
+        if (tid < 8) sh.elems[n[0] + tid] = 0ull;
+        __syncthreads();
     }
-    const uint32_t n = min(sh.n_elems, (uint32_t)kElemList);
-    if (tid < 8) sh.elems[n + tid] = 0ull;                 // the ranks are counted eight keys at a time
-    __syncthreads();
+
     const double ln_s = sh.ln_s;
     int32_t* ids = a.top_ids + row * a.K;
     float* logp = a.top_logp + row * a.K;
-    for (uint32_t j = tid; j < n; j += kTopkThreads) {
-        const uint64_t mine = sh.elems[j];
-        uint32_t rank = 0;
-        for (uint32_t i = 0; i < n; i += 8) {
+    uint32_t total = 0;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) rank += sh.elems[i + q] > mine ? 1u : 0u;
+    for (int w = 0; w < kTopkWaves; ++w) total += n[w];
+    // a key's rank is its place; with few keys two or four lanes count for each
+    const uint32_t lg_parts = total <= kTopkThreads / 4 ? 2 : total <= kTopkThreads / 2 ? 1 : 0;
+    const uint32_t part = (uint32_t)tid & ((1u << lg_parts) - 1u);
+    for (uint32_t j0 = 0; j0 < total; j0 += kTopkThreads >> lg_parts) {
+        const uint32_t j = j0 + ((uint32_t)tid >> lg_parts);
+        uint64_t key = 0;
+        uint32_t at = j;
+        if (j < total) {
+            uint32_t w = 0;
+            while (at >= n[w]) at -= n[w++];
+            key = sh.elems[w * kElemSlots + at];
         }
-        if (rank < K) {
-            ids[rank] = (int32_t)(0xffffffffu - (uint32_t)mine);
-            logp[rank] = (float)(((double)value_of((uint32_t)(mine >> 32)) - (double)st.m) * a.inv_t - ln_s);
+        uint32_t rank = 0;
+#pragma unroll
+        for (int w = 0; w < kTopkWaves; ++w) {
+            for (uint32_t i = part * 8; i < n[w]; i += 8u << lg_parts) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) rank += sh.elems[w * kElemSlots + i + q] > key ? 1u : 0u;
+            }
+        }
+        if (lg_parts >= 1) rank += (uint32_t)__builtin_amdgcn_mov_dpp((int)rank, kXor1, 0xF, 0xF, true);
+        if (lg_parts >= 2) rank += (uint32_t)__builtin_amdgcn_mov_dpp((int)rank, kXor2, 0xF, 0xF, true);
+        if (j < total && part == 0 && rank < K) {
+            ids[rank] = (int32_t)(0xffffffffu - (uint32_t)key);
+            logp[rank] = (float)(((double)value_of((uint32_t)(key >> 32)) - (double)st.m) * a.inv_t - ln_s);
         }
     }
-    for (uint32_t j = n + tid; j < K; j += kTopkThreads) {      // fewer unmasked tokens than were asked for
+    for (uint32_t j = total + tid; j < K; j += kTopkThreads) {      // fewer unmasked tokens than were asked for
         ids[j] = -1;
         logp[j] = -INFINITY;
     }
 }
 
-// One workgroup per row.  LG: log2 of the vectors in a group, kManyVectors: a.lg, more than a run of 16 lanes.
+// The stream over vectors [begin, end) of a row (begin and, unless it is the row's end, end whole groups): the lane's statistics,
+// and the groups' maxima in sh.gmax, from begin's group on, valid after a barrier.
+// LG: log2 of the vectors in a group, or kManyVectors: a.lg, more than a run of 16 lanes.
 constexpr int kManyVectors = 5;
 template <class Tr, int LG>
-__global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
+__device__ __forceinline__ Lane stream_vectors(const TopkArgs& a, const typename Tr::elem* rowp, int begin, int end, Shared& sh)
 {
     constexpr int NT = kTopkThreads, U = kTopkUnroll, E = Tr::kPerVec;
-    __shared__ Shared sh;
     const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x;
-    const typename Tr::elem* rowp = logits + row * a.row_stride;
-    const int nvec = a.V / E, all = (a.V + E - 1) / E;
-    const int ngroups = (all + (1 << a.lg) - 1) >> a.lg;
+    const int whole_end = min(a.V / E, end);        // where the whole vectors end
+    const int g0 = begin >> a.lg;
     if constexpr (LG == kManyVectors) {
-        for (int g = tid; g < ngroups; g += NT) sh.gmax[g] = kEmpty;
+        for (int g = tid; g <= ((end - 1) >> a.lg) - g0; g += NT) sh.gmax[g] = kEmpty;
         __syncthreads();
     }
     // the largest of each of this thread's four vectors, 256 apart from `first` on, into their groups'
@@ -460,21 +519,18 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
             for (int k = 0; k < 4; ++k) {
                 float g = vm[k];
                 if constexpr (LG == 1) g = larger(g, from_lane<kXor1>(g));
-                if (whole || first + k * NT + tid < all) sh.gmax[(first >> LG) + k * (NT >> LG) + (tid >> LG)] = g;
+                if (whole || first + k * NT + tid < end) sh.gmax[((first >> LG) - g0) + k * (NT >> LG) + (tid >> LG)] = g;
             }
         } else {
             constexpr int RUN = LG < 4 ? LG : 4;
             const float g = run_max4<RUN>(vm, tid);
             const int k = kept_vector<RUN>(tid), at = k * NT + (tid & -(1 << RUN));      // from first on
-            if (whole || first + at < all) {
-                if constexpr (LG == kManyVectors) atomicMax(&sh.gmax[(first + at) >> a.lg], g);
-                else sh.gmax[(first >> LG) + (at >> LG)] = g;
+            if (whole || first + at < end) {
+                if constexpr (LG == kManyVectors) atomicMax(&sh.gmax[((first + at) >> a.lg) - g0], g);
+                else sh.gmax[((first >> LG) - g0) + (at >> LG)] = g;
             }
         }
     };
-    const int32_t y = a.token_ids ? a.token_ids[row] : -1;
-    const bool has_y = y >= 0 && y < a.V;
-    const float zy = has_y ? Tr::load1(rowp + y) : 0.0f;      // ahead of the stream, so that nothing waits for it at the end
     Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
     auto take = [&](const u32x4* v, int first, auto whole) {
         const u32x4 four[4] = {v[0], v[1], v[2], v[3]};
@@ -482,8 +538,8 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
         absorb_vectors<Tr, 4>(four, a.scale, acc, vm);
         note(vm, first, whole);
     };
-    int base = 0;
-    for (; base + U * NT <= nvec; base += U * NT) {
+    int base = begin;
+    for (; base + U * NT <= whole_end; base += U * NT) {
         u32x4 v[U];
 #pragma unroll
         for (int k = 0; k < U; ++k)      // uniform base, lane offset
@@ -492,26 +548,47 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
 #pragma unroll
         for (int k = 0; k < U; k += 4) take(v + k, base + k * NT, std::true_type{});
     }
-    if (base < all) {       // the rest, its loads together
+    if (base < end) {       // the rest, its loads together
         u32x4 v[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) v[k] = load_vector<Tr>(rowp, a.V, base + k * NT + tid);
+        for (int k = 0; k < U; ++k) v[k] = base + k * NT + tid < end ? load_vector<Tr>(rowp, a.V, base + k * NT + tid) : Tr::filler();
 #pragma unroll
         for (int k = 0; k < U; k += 4)
-            if (base + k * NT < all) take(v + k, base + k * NT, std::false_type{});
+            if (base + k * NT < end) take(v + k, base + k * NT, std::false_type{});
     }
-    const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
+    return acc;
+}
+
+// What a row's token has to do with its results, fetched ahead of what they are waited for with.
+struct Token {
+    bool has;
+    float z;
+};
+template <class Tr>
+__device__ __forceinline__ Token token_of(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row)
+{
+    const int32_t y = a.token_ids ? a.token_ids[row] : -1;
+    const bool has = y >= 0 && y < a.V;
+    return Token{has, has ? Tr::load1(rowp + y) : 0.0f};
+}
+
+// A row's results from its statistics and its groups' maxima in sh.gmax.  All threads call it after a barrier.
+template <class Tr>
+__device__ __forceinline__ void finish_row(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, const Row& st, const Token& token, Shared& sh)
+{
+    constexpr int E = Tr::kPerVec;
+    const int all = (a.V + E - 1) / E, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
     const bool ok = st.m > kFloor && st.S >= 0.5 && st.S < 1.0e30;       // neither NaN, +infinity nor everything masked
-    if (tid == 0) {
+    if (threadIdx.x == 0) {
         const double ln_s = log(st.S);
         sh.ln_s = ln_s;
         const float nan = __builtin_nanf("");
         a.lse[row] = ok ? (float)((double)st.m * a.inv_t + ln_s) : nan;
         a.entropy[row] = ok ? (float)(ln_s - st.T * (double)kLn2 / st.S) : nan;
-        if (a.logp) a.logp[row] = ok && has_y ? (float)(((double)zy - (double)st.m) * a.inv_t - ln_s) : nan;
+        if (a.logp) a.logp[row] = ok && token.has ? (float)(((double)token.z - (double)st.m) * a.inv_t - ln_s) : nan;
     }
     if (!ok) {
-        for (int j = tid; j < a.K; j += NT) {
+        for (int j = threadIdx.x; j < a.K; j += kTopkThreads) {
             a.top_ids[row * a.K + j] = -1;
             a.top_logp[row * a.K + j] = __builtin_nanf("");
         }
@@ -520,21 +597,112 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
     select_and_write<Tr>(a, rowp, row, ngroups, st, sh);
 }
 
-template <class Tr>
-void launch_topk_rows(const void* logits, const TopkArgs& a, hipStream_t st)
+// Rows over grid dimensions x and y: a launch holds at most 2^32 threads along one.
+constexpr int64_t kRowsPerGridX = 1 << 20;
+__device__ __forceinline__ int64_t row_of_grid() { return (int64_t)blockIdx.y * kRowsPerGridX + blockIdx.x; }
+
+// One workgroup per row.  At 151936 bf16 logits and K 64 it reads 6.4 TB/s (the statistics alone: 7.0): its vector ALUs are
+// 85 % busy, the search adds 10 % of instructions (K 128: 25 %) and 7 us in which a workgroup loads little; four workgroups share a
+// compute unit (five, with registers in scratch memory for it, 20 % slower; 12 loads in flight instead of 8, three workgroups, 2 %).
+template <class Tr, int LG>
+__global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
 {
-    auto go = [&](auto lg) {
-        constexpr int LG = decltype(lg)::value;
-        hipLaunchKernelGGL((topk_row_kernel<Tr, LG>), dim3((unsigned)a.N), dim3(kTopkThreads), 0, st, (const typename Tr::elem*)logits, a);
-    };
-    switch (a.lg) {
-    case 0: return go(std::integral_constant<int, 0>{});
-    case 1: return go(std::integral_constant<int, 1>{});
-    case 2: return go(std::integral_constant<int, 2>{});
-    case 3: return go(std::integral_constant<int, 3>{});
-    case 4: return go(std::integral_constant<int, 4>{});
-    default: return go(std::integral_constant<int, kManyVectors>{});
+    __shared__ Shared sh;
+    const int64_t row = row_of_grid();
+    if (row >= a.N) return;
+    const typename Tr::elem* rowp = logits + row * a.row_stride;
+    const Token token = token_of<Tr>(a, rowp, row);
+    const Lane acc = stream_vectors<Tr, LG>(a, rowp, 0, (a.V + Tr::kPerVec - 1) / Tr::kPerVec, sh);
+    const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
+    finish_row<Tr>(a, rowp, row, st, token, sh);
+}
+
+// Few rows: several workgroups stream a row's pieces, one more finishes it.  What a row's pieces leave for it:
+struct RowParts {
+    float gmax[kMaxGroups];
+    Row piece[kMaxPieces];
+};
+template <class Tr, int LG>
+__global__ __launch_bounds__(kTopkThreads) void topk_piece_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a, RowParts* parts)
+{
+    __shared__ Shared sh;
+    const int64_t row = blockIdx.y;
+    const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
+    const int begin = (int)blockIdx.x * a.piece_vectors, end = min(all, begin + a.piece_vectors);
+    const Lane acc = stream_vectors<Tr, LG>(a, logits + row * a.row_stride, begin, end, sh);
+    const Row st = merge_lanes(acc, a.scale, sh);
+    RowParts& to = parts[row];
+    if (threadIdx.x == 0) to.piece[blockIdx.x] = st;
+    const int g0 = begin >> a.lg, g1 = (end - 1) >> a.lg;
+    for (int g = g0 + (int)threadIdx.x; g <= g1; g += kTopkThreads) to.gmax[g] = sh.gmax[g - g0];
+}
+template <class Tr>
+__global__ __launch_bounds__(kTopkThreads) void topk_merge_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a, int32_t pieces, const RowParts* parts)
+{
+    __shared__ Shared sh;
+    __shared__ Row merged;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const typename Tr::elem* rowp = logits + row * a.row_stride;
+    const RowParts& from = parts[row];
+    const Token token = token_of<Tr>(a, rowp, row);
+    const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
+#pragma unroll
+    for (int i = 0; i < kMaxGroups / kTopkThreads; ++i)
+        if (i * kTopkThreads + tid < ngroups) sh.gmax[i * kTopkThreads + tid] = from.gmax[i * kTopkThreads + tid];
+    if (tid < 64) {         // a piece per lane
+        static_assert(kMaxPieces == 64, "one piece per lane");
+        Row p = {kFloor, 0.0, 0.0};
+        if (tid < pieces) p = from.piece[tid];
+        const float m = wave_max(p.m);
+        const float d = (p.m - m) * a.scale;
+        const double s = (double)fast_exp2(d);
+        const double S = wave_sum_f64(s * p.S), T = wave_sum_f64(s * (p.T + (double)d * p.S));
+        if (tid == 0) merged = Row{m, S, T};
     }
+    __syncthreads();
+    const Row st = merged;
+    finish_row<Tr>(a, rowp, row, st, token, sh);
+}
+
+// f(constant) for the log2 of a group's vectors.
+template <class F>
+void with_group(int lg, const F& f)
+{
+    switch (lg) {
+    case 0: return f(std::integral_constant<int, 0>{});
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 3: return f(std::integral_constant<int, 3>{});
+    case 4: return f(std::integral_constant<int, 4>{});
+    default: return f(std::integral_constant<int, kManyVectors>{});
+    }
+}
+
+template <class Tr>
+void launch_topk(const void* logits, TopkArgs a, RowParts* parts, hipStream_t st)
+{
+    const typename Tr::elem* z = (const typename Tr::elem*)logits;
+    const int64_t all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
+    a.lg = 0;
+    while (((all + ((int64_t)1 << a.lg) - 1) >> a.lg) > kMaxGroups) ++a.lg;
+    // Pieces of whole batches of 1024 vectors, as many as bring the launch to about kFewWorkgroups workgroups.
+    const int64_t batch = 4 * kTopkThreads, batches = (all + batch - 1) / batch;
+    int64_t per = (batches * a.N + kFewWorkgroups - 1) / kFewWorkgroups;
+    if (per < (batches + kMaxPieces - 1) / kMaxPieces) per = (batches + kMaxPieces - 1) / kMaxPieces;
+    const int64_t pieces = (batches + per - 1) / per;
+    if (parts != nullptr && a.N <= kSplitRows && batches >= kSplitBatches && pieces > 1 && ((int64_t)1 << a.lg) <= batch) {
+        a.piece_vectors = (int32_t)(per * batch);
+        with_group(a.lg, [&](auto lg) {
+            hipLaunchKernelGGL((topk_piece_kernel<Tr, decltype(lg)::value>), dim3((unsigned)pieces, (unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, parts);
+        });
+        hipLaunchKernelGGL((topk_merge_kernel<Tr>), dim3((unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, (int32_t)pieces, parts);
+        return;
+    }
+    const dim3 grid((unsigned)(a.N < kRowsPerGridX ? a.N : kRowsPerGridX), (unsigned)((a.N + kRowsPerGridX - 1) / kRowsPerGridX));
+    with_group(a.lg, [&](auto lg) {
+        hipLaunchKernelGGL((topk_row_kernel<Tr, decltype(lg)::value>), grid, dim3(kTopkThreads), 0, st, z, a);
+    });
 }
 
 }  // namespace
@@ -544,7 +712,7 @@ extern "C" {
 size_t ulorl_token_topk_workspace_bytes(int64_t N, int64_t V)
 {
     if (!shape_ok(N, V, V) || N > 0x7fffffffLL) return 0;
-    return 256;
+    return (size_t)(N < kSplitRows ? N : kSplitRows) * sizeof(RowParts);
 }
 
 int32_t ulorl_token_topk(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t* token_ids,
@@ -564,14 +732,12 @@ int32_t ulorl_token_topk(const void* logits, int32_t dt, int64_t N, int64_t V, i
     a.N = N; a.row_stride = row_stride; a.V = (int32_t)V; a.K = K;
     a.inv_t = 1.0 / (double)temperature;
     a.scale = (float)(1.4426950408889634074 * a.inv_t);
-    const int64_t all = (V + (dt == ULORL_F32 ? 3 : 7)) / (dt == ULORL_F32 ? 4 : 8);
-    a.lg = 0;
-    while (((all + ((int64_t)1 << a.lg) - 1) >> a.lg) > kMaxGroups) ++a.lg;
+    a.lg = 0; a.piece_vectors = 0;
     hipStream_t st = (hipStream_t)hip_stream;
     if (dt == ULORL_BF16)
-        launch_topk_rows<StoreBF16>(logits, a, st);
+        launch_topk<StoreBF16>(logits, a, (RowParts*)workspace, st);
     else
-        launch_topk_rows<StoreF32>(logits, a, st);
+        launch_topk<StoreF32>(logits, a, (RowParts*)workspace, st);
     return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
 }
 
