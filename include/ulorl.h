@@ -77,6 +77,7 @@ enum {
     ULORL_STATUS_BAD_TOKEN = 1,     /* a token id outside [0, V)                      */
     ULORL_STATUS_NONFINITE = 2,     /* a row whose softmax statistics are not finite  */
     ULORL_STATUS_BAD_CU = 4,        /* cu_seqlens not 0 = cu[0] <= ... <= cu[R] = N   */
+    ULORL_STATUS_BAD_TARGET = 16,   /* distillation: a row whose target is no distribution (see there) */
     ULORL_STATUS_SYNC = 8           /* one-call path only, informational: a workgroup waited in vain
                                        (seconds; never observed) for the others that share its row.
                                        It then wrote nothing; the call's repair pass finished its
@@ -321,6 +322,73 @@ int32_t ulorl_token_topk(
     const void *logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t *token_ids,
     int32_t K, float temperature, int32_t *top_ids, float *top_logp, float *logp, float *entropy, float *lse,
     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Distillation from a teacher's recorded tokens (what ulorl_token_topk writes of the teacher's logits).
+ * A row's target is a distribution over its K listed tokens and one bucket for all others.  With
+ * x = z / temperature, p = softmax(x) and "rest" the tokens that are not listed:
+ *   q_k, q_rest   BUCKET  q_k = e^teacher_logp_k, q_rest = max(0, 1 - sum q_k): the others as one event
+ *                 RENORM  q = softmax over the listed values (which may be logits, or lack a constant), q_rest = 0
+ *                 DROP    q_k = e^teacher_logp_k, q_rest = 0: the teacher's other mass is left out
+ *                 teacher_logp is taken as it is: recorded at the temperature of the distillation.
+ *   kl_t          = sum_k q_k (ln q_k - ln p_k) + q_rest (ln q_rest - ln p_rest)
+ *   loss          = (1/D) sum_t weight_t kl_t
+ *   dlogits       listed: g (Q p_k - q_k), unlisted: g (Q p_rest - q_rest) e^(x_j) / sum_rest e^x, with
+ *                 g = grad_out weight_t / (D temperature), Q = sum q_k + q_rest.  Nothing else has a gradient.
+ *
+ *   logits, dt, N, V, row_stride   as in ulorl_token_loss_fwd, N <= 2^24; a logit at or below -9e29 (-infinity
+ *                 included) is masked: probability 0, gradient 0.  A lone row (N = 1) needs no particular row_stride.
+ *   teacher_ids   [N, K] int32, 1 <= K <= 128, distinct within a row, in any order; negative: no entry
+ *   teacher_logp  [N, K] (that of a missing entry is not looked at; -infinity: listed with probability 0)
+ *   weights       [N] or NULL (all 1).  A row of weight 0 (prompt, padding) is not read, whatever it holds, and
+ *                 gets a zero gradient.
+ * Outputs (DEVICE):
+ *   loss [1], kl [N], lse [N] (ln sum e^x of the row)
+ *   rest_max, rest_coef [N], top_grad [N, K]   what the backward call needs: the gradient of an unlisted token is
+ *                 rest_coef e^((z - rest_max) / temperature), that of a listed one top_grad, for a grad_out of 1
+ *   counters [4] int64, may be NULL: rows that count, rows of weight 0, rows that list nothing (all entries missing;
+ *                 RENORM: all of probability 0), status word
+ * Rows that do not count (kl, gradient and lse are 0): weight 0; nothing listed; and with a status bit an id >= V
+ * (ULORL_STATUS_BAD_TOKEN), an id twice, a log-prob that is not-a-number or +infinity, or a weight that is not finite
+ * (ULORL_STATUS_BAD_TARGET).  A row that has not-a-number or +infinity among its logits, nothing unmasked, or a masked
+ * token to which the teacher gives probability raises ULORL_STATUS_NONFINITE: kl and gradient 0, lse as it comes.
+ *   workspace     >= ulorl_distill_workspace_bytes(N, V, dt) bytes, 256-byte aligned; need not be preserved.
+ *
+ * ulorl_distill_fwd      loss and per-row outputs; one read of the logits
+ * ulorl_distill_bwd      dlogits from them; type and stride of logits, MAY BE THE SAME BUFFER.  grad_out: HOST scalar;
+ *                        grad_scale: DEVICE scalar that multiplies it, or NULL
+ * ulorl_distill_fwd_bwd  both
+ */
+enum { ULORL_TAIL_BUCKET = 0, ULORL_TAIL_RENORM = 1, ULORL_TAIL_DROP = 2 };
+
+typedef struct ulorl_distill_params {
+    float temperature;    /* in [1e-3, 1e3]                                                 */
+    int32_t tail;         /* ULORL_TAIL_*                                                    */
+    double denominator;   /* <= 0: D = N; > 0: this D                                       */
+    int32_t reserved[2];  /* must be 0                                                      */
+} ulorl_distill_params;
+
+size_t ulorl_distill_workspace_bytes(int64_t N, int64_t V, int32_t dt);
+
+int32_t ulorl_distill_fwd(
+    const void *logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride,
+    const int32_t *teacher_ids, const float *teacher_logp, int32_t K, const float *weights,
+    const ulorl_distill_params *p,
+    float *loss, float *kl, float *lse, float *rest_max, float *rest_coef, float *top_grad, int64_t *counters,
+    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+int32_t ulorl_distill_bwd(
+    const void *logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride,
+    const int32_t *teacher_ids, int32_t K, float temperature,
+    const float *rest_max, const float *rest_coef, const float *top_grad,
+    float grad_out, const float *grad_scale, void *dlogits, void *hip_stream);
+
+int32_t ulorl_distill_fwd_bwd(
+    const void *logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride,
+    const int32_t *teacher_ids, const float *teacher_logp, int32_t K, const float *weights,
+    const ulorl_distill_params *p, float grad_out,
+    float *loss, float *kl, float *lse, float *rest_max, float *rest_coef, float *top_grad, int64_t *counters,
+    void *dlogits, void *workspace, size_t workspace_bytes, const ulorl_launch *launch, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------------
  * lm_head variant: the logits are hidden . W and are never materialised.

@@ -26,7 +26,7 @@ from typing import Optional
 import torch
 
 from . import binding
-from .binding import FwdResult, Launch, Params
+from .binding import DistillParams, DistillResult, FwdResult, Launch, Params
 
 
 class _FusedTokenLoss(torch.autograd.Function):
@@ -83,4 +83,41 @@ def lmhead_token_loss(hidden: torch.Tensor, weight: torch.Tensor, token_ids, cu_
     return loss
 
 
-__all__ = ["token_loss", "lmhead_token_loss", "FwdResult"]
+class _FusedDistill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, teacher_ids, teacher_logp, weights, params, in_place, launch, sink):
+        res, ctx.dlogits = binding.distill_fwd_bwd(logits, teacher_ids, teacher_logp, weights, params, grad_out=1.0, inplace=bool(in_place),
+                                                   launch=launch)
+        if sink is not None:
+            sink.append(res)
+        return res.loss.reshape(())
+
+    @staticmethod
+    def backward(ctx, grad_loss):
+        g = float(grad_loss)
+        if g != 1.0:
+            raise RuntimeError("distill_loss(fused=True) computed the gradient of an upstream 1 in its forward pass; "
+                               "got an upstream gradient of %r: scale through DistillParams.denominator or use fused=False" % g)
+        d = ctx.dlogits
+        ctx.dlogits = None
+        return (d,) + (None,) * 7
+
+
+def distill_loss(logits: torch.Tensor, teacher_ids, teacher_logp, weights=None, params: Optional[DistillParams] = None,
+                 fused: bool = False, in_place: bool = False, launch: Optional[Launch] = None,
+                 results: Optional[list] = None) -> torch.Tensor:
+    """The weighted mean divergence of each row from its teacher's listed tokens as a differentiable 0-dim tensor (gradient to
+    ``logits`` only).  ``fused`` and ``in_place`` as in ``token_loss``; ``results``: a list that receives the call's
+    ``DistillResult``."""
+    if fused:
+        return _FusedDistill.apply(logits, teacher_ids, teacher_logp, weights, params, in_place, launch, results)
+    if in_place:
+        raise ValueError("in_place needs fused=True (the two-call path reads the logits again in backward)")
+    c = (params or DistillParams()).to_c()
+    loss, fields = binding.native().autograd_distill(logits, teacher_ids, teacher_logp, weights, binding._addr(c), results is not None)
+    if results is not None:
+        results.append(DistillResult(*fields))
+    return loss
+
+
+__all__ = ["token_loss", "lmhead_token_loss", "distill_loss", "FwdResult", "DistillResult"]

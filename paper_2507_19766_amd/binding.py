@@ -18,7 +18,8 @@ import torch
 F32, BF16 = 0, 1
 IS_SAIS, IS_POIS = 0, 1
 GATE_PER_RESPONSE, GATE_GLOBAL, GATE_ALWAYS, GATE_NEVER = 0, 1, 2, 3
-STATUS_BAD_TOKEN, STATUS_NONFINITE, STATUS_BAD_CU, STATUS_SYNC = 1, 2, 4, 8
+STATUS_BAD_TOKEN, STATUS_NONFINITE, STATUS_BAD_CU, STATUS_SYNC, STATUS_BAD_TARGET = 1, 2, 4, 8, 16
+TAIL_BUCKET, TAIL_RENORM, TAIL_DROP = 0, 1, 2
 LAUNCH_PER_ROW = 1
 LAUNCH_DENSE_ROWS = 2
 
@@ -42,6 +43,11 @@ class _CParams(ctypes.Structure):
 class _CLaunch(ctypes.Structure):
     _fields_ = [("flags", ctypes.c_uint32), ("sync_spins", ctypes.c_int32), ("gemm_tile", ctypes.c_int32),
                 ("gemm_group_m", ctypes.c_int32), ("reserved", ctypes.c_int32 * 4)]
+
+
+class _CDistillParams(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("tail", ctypes.c_int32), ("denominator", ctypes.c_double),
+                ("reserved", ctypes.c_int32 * 2)]
 
 
 class _CSegStats(ctypes.Structure):
@@ -158,6 +164,16 @@ def load_library(build_if_missing: bool = True):
     lib.ulorl_token_topk.restype = c.c_int32
     lib.ulorl_token_topk.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int64, vp, c.c_int32, c.c_float,
                                      vp, vp, vp, vp, vp, vp, c.c_size_t, vp]
+    lib.ulorl_distill_workspace_bytes.restype = c.c_size_t
+    lib.ulorl_distill_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int32]
+    lib.ulorl_distill_fwd.restype = c.c_int32
+    lib.ulorl_distill_fwd.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int64, vp, vp, c.c_int32, vp, c.POINTER(_CDistillParams),
+                                      vp, vp, vp, vp, vp, vp, vp, vp, c.c_size_t, vp]
+    lib.ulorl_distill_bwd.restype = c.c_int32
+    lib.ulorl_distill_bwd.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int64, vp, c.c_int32, c.c_float, vp, vp, vp, c.c_float, vp, vp, vp]
+    lib.ulorl_distill_fwd_bwd.restype = c.c_int32
+    lib.ulorl_distill_fwd_bwd.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int64, vp, vp, c.c_int32, vp, c.POINTER(_CDistillParams),
+                                          c.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp, c.c_size_t, vp, vp]
     lib.ulorl_lmhead_workspace_bytes.restype = c.c_size_t
     lib.ulorl_lmhead_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int64, c.c_int32, c.c_int32]
     lib.ulorl_lmhead_token_loss_fwd.restype = c.c_int32
@@ -357,6 +373,69 @@ def token_topk(logits, k: int, token_ids=None, temperature: float = 1.0, out: Op
     given = None if out is None else [out.top_ids, out.top_logp, out.logp, out.entropy, out.lse]
     fields = native().token_topk(logits, int(k), token_ids, float(temperature), given, workspace)
     return TopkResult(*fields)
+
+
+# ------------------------------------------------------------------------------------ distillation
+
+@dataclass
+class DistillParams:
+    """Temperature of both sides (``teacher_logp`` is taken as recorded at it), what becomes of the teacher's mass outside the
+    listed tokens, and D of the mean (0: the number of rows)."""
+    temperature: float = 1.0
+    tail: int = TAIL_BUCKET
+    denominator: float = 0.0
+
+    def to_c(self) -> _CDistillParams:
+        return _CDistillParams(self.temperature, self.tail, self.denominator, (ctypes.c_int32 * 2)(0, 0))
+
+
+@dataclass
+class DistillResult:
+    """Loss [1], divergence and log-sum-exp of each row [N], what ``distill_bwd`` needs (``rest_max``, ``rest_coef`` [N],
+    ``top_grad`` [N, K]) and four counters: rows that count, rows of weight 0, rows that list nothing, status word."""
+    loss: torch.Tensor
+    kl: torch.Tensor
+    lse: torch.Tensor
+    rest_max: torch.Tensor
+    rest_coef: torch.Tensor
+    top_grad: torch.Tensor
+    counters: torch.Tensor
+
+
+def _distill_given(out: Optional[DistillResult]):
+    return None if out is None else [out.loss, out.kl, out.lse, out.rest_max, out.rest_coef, out.top_grad, out.counters]
+
+
+def distill_workspace_bytes(N: int, V: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    return int(load_library().ulorl_distill_workspace_bytes(N, V, F32 if dtype == torch.float32 else BF16))
+
+
+def distill_fwd(logits, teacher_ids, teacher_logp, weights=None, params: Optional[DistillParams] = None, out: Optional[DistillResult] = None,
+                workspace: Optional[torch.Tensor] = None) -> DistillResult:
+    """ulorl_distill_fwd: divergence of each row's softmax from the teacher's listed tokens (``token_topk``'s, say) and their
+    weighted mean.  ``out``/``workspace`` let a caller reuse buffers."""
+    c = (params or DistillParams()).to_c()
+    return DistillResult(*native().distill_fwd(logits, teacher_ids, teacher_logp, weights, _addr(c), _distill_given(out), workspace))
+
+
+def distill_bwd(logits, teacher_ids, res: DistillResult, params: Optional[DistillParams] = None, grad_out: float = 1.0,
+                grad_scale: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, inplace: bool = False) -> torch.Tensor:
+    """ulorl_distill_bwd on the result of a forward call.  ``grad_scale``: a device scalar that multiplies ``grad_out``;
+    ``inplace=True`` overwrites ``logits`` with the gradient."""
+    temperature = (params or DistillParams()).temperature
+    return native().distill_bwd(logits, teacher_ids, res.rest_max, res.rest_coef, res.top_grad, float(temperature), float(grad_out),
+                                grad_scale, dlogits, bool(inplace))
+
+
+def distill_fwd_bwd(logits, teacher_ids, teacher_logp, weights=None, params: Optional[DistillParams] = None, grad_out: float = 1.0,
+                    dlogits: Optional[torch.Tensor] = None, inplace: bool = False, out: Optional[DistillResult] = None,
+                    workspace: Optional[torch.Tensor] = None, launch: Optional[Launch] = None):
+    """ulorl_distill_fwd_bwd -> (DistillResult, dlogits).  ``inplace=True`` overwrites ``logits``."""
+    c = (params or DistillParams()).to_c()
+    with_launch = launch.to_c() if launch is not None else None
+    fields, d = native().distill_fwd_bwd(logits, teacher_ids, teacher_logp, weights, _addr(c), float(grad_out), dlogits, bool(inplace),
+                                         _distill_given(out), workspace, _addr(with_launch))
+    return DistillResult(*fields), d
 
 
 # ------------------------------------------------------------------------------------ lm_head variant

@@ -1,0 +1,669 @@
+// Distillation from a teacher's recorded tokens: ulorl_distill_fwd / _bwd / _fwd_bwd.
+//
+// A row's target is a distribution over the listed tokens and one bucket for all others.  With x = z / T, p = softmax(x), q_k the
+// teacher's probabilities, q_rest what it leaves to the others, Q = sum q_k + q_rest, and "rest" the unlisted tokens:
+//     kl      = sum_k q_k (ln q_k - ln p_k) + q_rest (ln q_rest - ln p_rest)
+//     d kl / d x_k (listed)   = p_k Q - q_k
+//     d kl / d x_j (unlisted) = (Q p_rest - q_rest) softmax_rest(j),    softmax_rest(j) = e^(x_j) / sum_rest e^x
+// So the vocabulary enters a row by two numbers, the largest unlisted logit and the sum S over the unlisted ones relative to it;
+// the listed logits are K numbers that are gathered on the way.  S leaves the listed tokens out while it is formed: p_rest as 1 minus
+// the listed probabilities would lose all its digits where the student is sure of them.  What a row is made of after that (K terms)
+// is in 64 bits: a divergence is a small sum of larger terms.
+//
+//   distill_target_kernel   one wave per row: is the target a distribution; what the row's gradient needs of it
+//   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers, to (max, S); listed logits
+//   distill_finish_kernel   one wave per row: kl, the listed tokens' gradients, the unlisted ones' coefficient; the loss
+//   distill_dense_kernel    the gradient of all tokens as if unlisted, one 16-byte vector per thread
+//   distill_top_kernel      the listed tokens' gradients over it
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "logits_stream.hpp"
+#include "row_sums.hpp"
+#include "ulorl.h"
+#include "ulorl_internal.hpp"
+
+using namespace ulorl_detail;
+
+#pragma clang fp contract(off)
+
+namespace {
+
+constexpr int kMaxK = 128;              // two listed tokens per lane of a wave
+constexpr int64_t kMaxDistillRows = 1 << 24;
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kFinishGroups = 1024;     // workgroups of the finishing kernel at most, each with its partial sums
+
+enum { ROW_ON = 0, ROW_WEIGHTLESS = 1, ROW_EMPTY = 2, ROW_BAD_TOKEN = 3, ROW_BAD_TARGET = 4 };
+
+// What the stream has to know of a row's target: g Q and g q_rest, with g = weight / (D T).
+struct RowTarget {
+    float mass, rest;
+    int32_t state;
+    int32_t unused;
+};
+
+struct Partial {
+    double loss;
+    int64_t on, weightless, empty, status;
+};
+
+struct DistillArgs {
+    const int32_t* ids;         // [N, K]
+    const float* teacher;       // [N, K]
+    const float* weights;       // may be NULL
+    float* loss;
+    float* kl;
+    float* lse;
+    float* rest_max;
+    float* rest_coef;
+    float* top_grad;            // [N, K]; the listed logits until the row is finished
+    int64_t* counters;          // may be NULL
+    RowTarget* target;          // [N]
+    unsigned long long* slots;  // [N * C * 2]: {max, S} of a piece's unlisted logits, {max, S} of its listed ones
+    Partial* partial;           // [kFinishGroups]
+    uint32_t* ticket;
+    int64_t N, row_stride;
+    int32_t V, K, C;
+    int32_t tail;
+    float scale;                // log2(e) / T
+    double inv_t, inv_D;
+};
+
+// Two values per lane of a wave, listed tokens lane and lane + 64.
+__device__ __forceinline__ double wave_sum2(double a, double b) { return wave_sum_f64(a + b); }
+
+// ---------------------------------------------------------------------------------------------
+// the targets
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
+
+__global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0u;
+    if (row >= a.N) return;
+    const float w = a.weights ? a.weights[row] : 1.0f;
+    int32_t id[2];
+    float l[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int j = lane + 64 * h;
+        id[h] = j < a.K ? a.ids[row * a.K + j] : -1;
+        l[h] = id[h] >= 0 ? a.teacher[row * a.K + j] : -INFINITY;
+    }
+    RowTarget t = {0.0f, 0.0f, ROW_ON, 0};
+    if (w == 0.0f) {
+        t.state = ROW_WEIGHTLESS;
+    } else {
+        // an id twice: every lane counts its own among all
+        uint32_t twice = 0;
+        const int n0 = a.K < 64 ? a.K : 64, n1 = a.K - n0;
+        uint32_t seen0 = 0, seen1 = 0;
+        for (int s = 0; s < n0; ++s) {
+            const int32_t other = __builtin_amdgcn_readlane(id[0], s);
+            seen0 += id[0] == other ? 1u : 0u;
+            seen1 += id[1] == other ? 1u : 0u;
+        }
+        for (int s = 0; s < n1; ++s) {
+            const int32_t other = __builtin_amdgcn_readlane(id[1], s);
+            seen0 += id[0] == other ? 1u : 0u;
+            seen1 += id[1] == other ? 1u : 0u;
+        }
+        twice = (id[0] >= 0 && seen0 > 1) || (id[1] >= 0 && seen1 > 1);
+        const bool beyond = id[0] >= a.V || id[1] >= a.V;
+        const bool bad = twice || !finite(w) || (id[0] >= 0 && !(l[0] <= 3.4028235e38f)) || (id[1] >= 0 && !(l[1] <= 3.4028235e38f));
+        if (__any(beyond)) {
+            t.state = ROW_BAD_TOKEN;
+        } else if (__any(bad)) {
+            t.state = ROW_BAD_TARGET;
+        } else if (!__any(id[0] >= 0 || id[1] >= 0) || (a.tail == ULORL_TAIL_RENORM && !__any(l[0] > -INFINITY || l[1] > -INFINITY))) {
+            t.state = ROW_EMPTY;
+        } else {
+            const double g = (double)w * a.inv_D * a.inv_t;
+            double mass = 1.0, rest = 0.0;
+            if (a.tail != ULORL_TAIL_RENORM) {
+                const double q = wave_sum2(exp((double)l[0]), exp((double)l[1]));
+                rest = a.tail == ULORL_TAIL_BUCKET && q < 1.0 ? 1.0 - q : 0.0;
+                mass = q + rest;
+            }
+            t.mass = (float)(g * mass);
+            t.rest = (float)(g * rest);
+        }
+    }
+    if (lane == 0) a.target[row] = t;
+}
+
+// ---------------------------------------------------------------------------------------------
+// the stream
+// ---------------------------------------------------------------------------------------------
+// Takes element e out of a vector: a masked logit in its place.
+template <class Tr>
+__device__ __forceinline__ void take_out(u32x4& v, int e)
+{
+    if constexpr (Tr::kPerVec == 8) {
+        const uint32_t keep = (e & 1) ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (w == (e >> 1)) v[w] = (v[w] & keep) | (Tr::filler()[0] & ~keep);
+    } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (w == e) v[w] = Tr::filler()[0];
+    }
+}
+
+// Absorbs vectors v[K .. VPT) in groups of four, two and one.
+template <class Tr, int VPT, int K>
+__device__ __forceinline__ void absorb_rest(const u32x4 (&v)[VPT], float scale, Lane& acc)
+{
+    constexpr int REM = VPT - K;
+    if constexpr (REM > 0) {
+        constexpr int G = REM >= 4 ? 4 : REM >= 2 ? 2 : 1;
+        constexpr int E = Tr::kPerVec;
+        float f[G * E];
+        float cm = kFloor;
+#pragma unroll
+        for (int q = 0; q < G; ++q) Tr::unpack(v[K + q], f + q * E);
+#pragma unroll
+        for (int k = 0; k < G * E; ++k) cm = larger(cm, f[k]);
+        absorb_scaled<G * E, false>(f, cm, scale, acc);
+        absorb_rest<Tr, VPT, K + G>(v, scale, acc);
+    }
+}
+
+struct PieceShared {
+    int32_t head[kThreads];     // of a thread's listed tokens, -1: none
+    int32_t next[kMaxK];
+    int32_t where[kMaxK];       // vector of the thread * 8 + element
+    float m[kWaves], top_m[kWaves];
+    double S[kWaves], top_S[kWaves];
+};
+
+struct PieceSums {
+    float m, top_m;
+    double S, top_S;            // relative to them
+};
+
+// A row's piece c into registers (v) without its listed tokens, whose logits go to a.top_grad, and its sums (thread 0).
+template <class Tr, int VPT>
+__device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT], PieceShared& sh)
+{
+    constexpr int NT = kThreads, E = Tr::kPerVec;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int nvec = a.V / E;
+    const int first = c * NT * VPT;
+    const int32_t id = tid < a.K ? a.ids[row * a.K + tid] : -1;
+    if (first + NT * VPT <= nvec) {
+        const char* const piece = reinterpret_cast<const char*>(rowp) + ((size_t)first << 4);
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) v[k] = load_stream(reinterpret_cast<const u32x4*>(piece + (size_t)k * NT * 16 + ((uint32_t)tid << 4)));
+    } else {
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) v[k] = load_vector<Tr>(rowp, a.V, first + k * NT + tid);
+    }
+
+    // each thread's listed tokens as a chain in LDS
+    sh.head[tid] = -1;
+    __syncthreads();
+    float z = kFloor;
+    bool dead = false;
+    {
+        const int at = id / E - first;              // id < V: the row's state says so
+        if (id >= 0 && at >= 0 && at < NT * VPT) {
+            z = Tr::load1(rowp + id);
+            a.top_grad[row * a.K + tid] = z;
+            sh.where[tid] = (at / NT) * 8 + (id & (E - 1));
+            sh.next[tid] = atomicExch(&sh.head[at & (NT - 1)], tid);
+            dead = z <= kFloor && a.teacher[row * a.K + tid] > -INFINITY;       // the teacher's token is masked here
+        }
+    }
+    __syncthreads();
+    for (int j = sh.head[tid]; j >= 0; j = sh.next[j]) {
+        const int k_j = sh.where[j] >> 3, e = sh.where[j] & 7;
+#pragma unroll
+        for (int k = 0; k < VPT; ++k)
+            if (k == k_j) take_out<Tr>(v[k], e);
+    }
+
+    Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
+    absorb_rest<Tr, VPT, 0>(v, a.scale, acc);
+    const float wm = wave_max(acc.m), wt = wave_max(z);
+    // z scale - mL differs from (z - m) scale by the rounding of mL: taken out here (nothing to take out of an empty lane)
+    const float d = fmaf(acc.m - wm, a.scale, -fmaf(acc.m, a.scale, -acc.mL));
+    const double S = acc.S == 0.0f ? 0.0 : (double)fast_exp2(d) * ((double)acc.S + (double)acc.Sc);
+    double top = z > kFloor ? (double)fast_exp2((z - wt) * a.scale) : 0.0;
+    if (z != z || dead) top = (double)__builtin_nanf("");
+    const double wS = wave_sum_f64(S), wT = wave_sum_f64(top);
+    if ((tid & 63) == 0) {
+        sh.m[wave] = wm;
+        sh.S[wave] = wS;
+        sh.top_m[wave] = wt;
+        sh.top_S[wave] = wT;
+    }
+    __syncthreads();
+    PieceSums p = {sh.m[0], sh.top_m[0], 0.0, 0.0};
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            p.m = larger(p.m, sh.m[w]);
+            p.top_m = larger(p.top_m, sh.top_m[w]);
+        }
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            p.S += (double)fast_exp2((sh.m[w] - p.m) * a.scale) * sh.S[w];
+            p.top_S += (double)fast_exp2((sh.top_m[w] - p.top_m) * a.scale) * sh.top_S[w];
+        }
+    }
+    return p;
+}
+
+// Never 0: a maximum is kFloor where there is nothing, and a sum is 1 or more where the maximum is 0.
+__device__ __forceinline__ unsigned long long slot_word(float m, double S)
+{
+    return ((unsigned long long)__float_as_uint((float)S) << 32) | __float_as_uint(m);
+}
+
+template <class Tr, int VPT>
+__global__ __launch_bounds__(kThreads) void distill_piece_kernel(const typename Tr::elem* logits, DistillArgs a)
+{
+    __shared__ PieceShared sh;
+    const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
+    if (row >= a.N || a.target[row].state != ROW_ON) return;
+    u32x4 v[VPT];
+    const PieceSums p = piece_sums<Tr, VPT>(a, logits + row * a.row_stride, row, (int)blockIdx.x, v, sh);
+    if (threadIdx.x == 0) {
+        unsigned long long* slot = a.slots + (row * a.C + blockIdx.x) * 2;
+        slot[0] = slot_word(p.m, p.S);
+        slot[1] = slot_word(p.top_m, p.top_S);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// the rows' results
+// ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a)
+{
+    __shared__ Partial part[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Partial mine = {0.0, 0, 0, 0, 0};
+    for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.N; row += (int64_t)gridDim.x * kWaves) {
+        const int32_t state = a.target[row].state;
+        float* top = a.top_grad + row * a.K;
+        float grad[2] = {0.0f, 0.0f};
+        float kl_out = 0.0f, lse_out = 0.0f, max_out = 0.0f, coef_out = 0.0f;
+        if (state == ROW_ON) {
+            // the unlisted tokens: the row's pieces
+            float m = kFloor;
+            double S = 0.0;
+            for (int c = lane; c < a.C; c += 64) {
+                const unsigned long long w0 = a.slots[(row * a.C + c) * 2];
+                const float pm = __uint_as_float((uint32_t)w0);
+                const float M = larger(m, pm);
+                S = exp((double)(m - M) * a.inv_t) * S + exp((double)(pm - M) * a.inv_t) * (double)__uint_as_float((uint32_t)(w0 >> 32));
+                m = M;
+            }
+            const float rest_max = wave_max(m);
+            S = wave_sum_f64(exp((double)(m - rest_max) * a.inv_t) * S);
+            // the listed ones
+            double z[2], l[2];
+            bool here[2], masked[2];
+            float M = rest_max;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = lane + 64 * h;
+                here[h] = j < a.K && a.ids[row * a.K + j] >= 0;
+                const float zf = here[h] ? top[j] : kFloor;
+                masked[h] = zf <= kFloor;
+                z[h] = (double)zf;
+                l[h] = here[h] ? (double)a.teacher[row * a.K + j] : -INFINITY;
+                M = larger(M, zf);
+            }
+            M = wave_max(M);
+            double e[2], q[2], lp[2], terms = 0.0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) e[h] = masked[h] ? 0.0 : exp((z[h] - (double)M) * a.inv_t);
+            const double total = exp((double)(rest_max - M) * a.inv_t) * S + wave_sum2(e[0], e[1]);
+            const double ln_total = log(total);
+            if (a.tail == ULORL_TAIL_RENORM) {
+                const double lm = (double)wave_max(larger((float)l[0], (float)l[1]));
+                const double norm = lm + log(wave_sum2(exp(l[0] - lm), exp(l[1] - lm)));
+                l[0] -= norm;
+                l[1] -= norm;
+            }
+            bool dead = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                q[h] = exp(l[h]);
+                lp[h] = (z[h] - (double)M) * a.inv_t - ln_total;
+                dead = dead || (here[h] && masked[h] && l[h] > -INFINITY);
+                if (q[h] > 0.0 && !masked[h]) terms += q[h] * (l[h] - lp[h]);
+            }
+            const double q_sum = wave_sum2(q[0], q[1]);
+            const bool has_rest = S > 0.0;
+            const double q_rest = a.tail == ULORL_TAIL_BUCKET && has_rest && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
+            const double mass = q_sum + q_rest;
+            const double ln_rest = (double)(rest_max - M) * a.inv_t + log(S) - ln_total;
+            double kl = wave_sum_f64(terms);
+            if (q_rest > 0.0) kl += q_rest * (log(q_rest) - ln_rest);
+            const bool ok = !__any(dead) && total > 0.0 && total < 1.0e300 && fabs(kl) < 1.0e300;
+            const double w = a.weights ? (double)a.weights[row] : 1.0;
+            const double g = w * a.inv_D * a.inv_t;
+            lse_out = total > 0.0 ? (float)((double)M * a.inv_t + ln_total) : __builtin_nanf("");
+            max_out = rest_max;
+            if (ok) {
+                kl_out = (float)kl;
+                if (has_rest) coef_out = (float)(g * (mass * exp(ln_rest) - q_rest) / S);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) grad[h] = here[h] ? (float)(g * ((masked[h] ? 0.0 : exp(lp[h])) * mass - q[h])) : 0.0f;
+                mine.loss += w * kl;
+                mine.on += 1;
+            } else {
+                max_out = 0.0f;
+                mine.status |= ULORL_STATUS_NONFINITE;
+            }
+        } else if (state == ROW_WEIGHTLESS) {
+            mine.weightless += 1;
+        } else if (state == ROW_EMPTY) {
+            mine.empty += 1;
+        } else {
+            mine.status |= state == ROW_BAD_TOKEN ? ULORL_STATUS_BAD_TOKEN : ULORL_STATUS_BAD_TARGET;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (lane + 64 * h < a.K) top[lane + 64 * h] = grad[h];
+        if (lane == 0) {
+            a.kl[row] = kl_out;
+            a.lse[row] = lse_out;
+            a.rest_max[row] = max_out;
+            a.rest_coef[row] = coef_out;
+        }
+    }
+    if (lane == 0) part[wave] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        Partial sum = {0.0, 0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            sum.loss += part[w].loss;
+            sum.on += part[w].on;
+            sum.weightless += part[w].weightless;
+            sum.empty += part[w].empty;
+            sum.status |= part[w].status;
+        }
+        Partial& to = a.partial[blockIdx.x];
+        publish(&to.loss, sum.loss);
+        publish(&to.on, sum.on);
+        publish(&to.weightless, sum.weightless);
+        publish(&to.empty, sum.empty);
+        publish(&to.status, sum.status);
+    }
+    if (!last_workgroup(a.ticket, gridDim.x)) return;
+    // all sums in a fixed order: lanes over workgroups, then lanes, then waves
+    Partial q = {0.0, 0, 0, 0, 0};
+    for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads) {
+        const Partial& from = a.partial[b];
+        q.loss += published(&from.loss);
+        q.on += published(&from.on);
+        q.weightless += published(&from.weightless);
+        q.empty += published(&from.empty);
+        q.status |= published(&from.status);
+    }
+    q.loss = wave_sum_f64(q.loss);
+    q.on = (int64_t)wave_sum_f64((double)q.on);                     // below 2^53: exact
+    q.weightless = (int64_t)wave_sum_f64((double)q.weightless);
+    q.empty = (int64_t)wave_sum_f64((double)q.empty);
+    int64_t status = 0;
+#pragma unroll
+    for (int bit = 1; bit <= ULORL_STATUS_BAD_TARGET; bit <<= 1) status |= __any((q.status & bit) != 0) ? bit : 0;
+    q.status = status;
+    if (lane == 0) part[wave] = q;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        Partial sum = part[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            sum.loss += part[w].loss;
+            sum.on += part[w].on;
+            sum.weightless += part[w].weightless;
+            sum.empty += part[w].empty;
+            sum.status |= part[w].status;
+        }
+        *a.loss = (float)(sum.loss * a.inv_D);
+        if (a.counters) {
+            a.counters[0] = sum.on;
+            a.counters[1] = sum.weightless;
+            a.counters[2] = sum.empty;
+            a.counters[3] = sum.status;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// the gradient
+// ---------------------------------------------------------------------------------------------
+// A coefficient that leaves a row zeros: none, or one that is no number.
+__device__ __forceinline__ bool no_gradient(float c) { return c == 0.0f || !finite(c); }
+
+// rest_coef e^((z - rest_max) / T) of every token: 4 KB of one row per workgroup, the shape in which a read-and-write stream is
+// fastest here.  In bf16 c e^(x - m) = sign(c) 2^(z scale + log2|c| - m scale), one fused step and one exp2; in fp32, where the
+// rounding of that sum (|m scale| and |log2 c| are tens) would be ten units of the result, c 2^((z - m) scale).
+template <class Tr>
+__global__ __launch_bounds__(kThreads) void distill_dense_kernel(const typename Tr::elem* logits, int64_t N, int64_t row_stride, int32_t V, float scale,
+                                                                 const float* rest_max, const float* rest_coef, float grad_out,
+                                                                 const float* grad_scale, typename Tr::elem* dlogits)
+{
+    constexpr int E = Tr::kPerVec;
+    const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
+    if (row >= N) return;
+    const float c = rest_coef[row] * (grad_scale ? *grad_scale * grad_out : grad_out);
+    const typename Tr::elem* rowp = logits + row * row_stride;
+    typename Tr::elem* outp = dlogits + row * row_stride;
+    const int nvec = V / E, i = (int)blockIdx.x * kThreads + (int)threadIdx.x;
+    const bool none = no_gradient(c);
+    constexpr bool EXACT = E == 4;
+    const float m = rest_max[row], shift = none || EXACT ? 0.0f : fmaf(-m, scale, log2f(fabsf(c)));
+    if (i < nvec) {
+        u32x4 o = {0u, 0u, 0u, 0u};
+        if (!none) {
+            float f[E];
+            Tr::unpack(load_stream(reinterpret_cast<const u32x4*>(rowp) + i), f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[e] = EXACT ? c * fast_exp2((f[e] - m) * scale) : fast_exp2(fmaf(f[e], scale, shift));
+            o = Tr::pack(f);
+            if (!EXACT && c < 0.0f) o ^= Tr::sign_bits();
+        }
+        store_stream(reinterpret_cast<u32x4*>(outp) + i, o);
+    } else if (i == nvec) {
+        for (int j = nvec * E; j < V; ++j) {
+            float x = 0.0f;
+            if (!none) x = EXACT ? fabsf(c) * fast_exp2((Tr::load1(rowp + j) - m) * scale) : fast_exp2(fmaf(Tr::load1(rowp + j), scale, shift));
+            Tr::store1(outp + j, c < 0.0f ? -x : x);
+        }
+    }
+}
+
+template <class Tr>
+__global__ __launch_bounds__(kThreads) void distill_top_kernel(const int32_t* ids, const float* top_grad, int64_t N, int64_t row_stride, int32_t V,
+                                                               int32_t K, float grad_out, const float* grad_scale, typename Tr::elem* dlogits)
+{
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= N * K) return;
+    const int32_t id = ids[i];
+    if (id < 0 || id >= V) return;
+    const float g = top_grad[i] * (grad_scale ? *grad_scale * grad_out : grad_out);
+    Tr::store1(dlogits + (i / K) * row_stride + id, finite(g) ? g : 0.0f);
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+struct Layout {
+    size_t target, partial, ticket, slots, total;
+    ClusterShape shape;         // vectors per thread, pieces per row
+};
+
+Layout layout_of(int64_t N, int64_t V, int32_t dt)
+{
+    Layout l;
+    const int64_t E = dt == ULORL_F32 ? 4 : 8, all = (V + E - 1) / E;
+    l.shape = cluster_shape(all * E, dt);
+    if (l.shape.pieces == 0) {                      // more than 64 pieces: no limit to the two-pass path
+        l.shape.vpt = 15;
+        l.shape.pieces = (int)((all + kThreads * 15 - 1) / (kThreads * 15));
+    }
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    size_t off = 0;
+    l.ticket = off;  off += 256;
+    l.partial = off; off = up(off + sizeof(Partial) * kFinishGroups);
+    l.target = off;  off = up(off + sizeof(RowTarget) * (size_t)N);
+    l.slots = off;   off = up(off + 16 * (size_t)N * (size_t)l.shape.pieces);
+    l.total = off;
+    return l;
+}
+
+bool temperature_ok(float t) { return t >= 1.0e-3f && t <= 1.0e3f; }
+
+int32_t check_distill(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t& row_stride, const int32_t* ids, int32_t K)
+{
+    if (N == 1 && row_stride >= V) row_stride = (V + 7) / 8 * 8;       // a lone row has no stride
+    const int32_t rc = check_logits(logits, dt, N, V, row_stride);
+    if (rc != ULORL_OK) return rc;
+    if (N > kMaxDistillRows || K < 1 || K > kMaxK) return ULORL_ERR_SHAPE;
+    return ids ? ULORL_OK : ULORL_ERR_NULL;
+}
+
+template <class Tr>
+bool launch_pieces(const Layout& l, const void* logits, const DistillArgs& a, hipStream_t st)
+{
+    const dim3 grid = rows_grid((unsigned)a.C, a.N);
+#define ULORL_CASE(VPT_)                                                                                                          \
+    if (l.shape.vpt == VPT_) {                                                                                                    \
+        hipLaunchKernelGGL((distill_piece_kernel<Tr, VPT_>), grid, dim3(kThreads), 0, st, (const typename Tr::elem*)logits, a);   \
+        return true;                                                                                                              \
+    }
+    ULORL_CASE(4) ULORL_CASE(8) ULORL_CASE(13) ULORL_CASE(15)
+    if constexpr (Tr::kPerVec == 8) {
+        ULORL_CASE(6) ULORL_CASE(7) ULORL_CASE(11)
+    } else {
+        ULORL_CASE(20)
+    }
+#undef ULORL_CASE
+    return false;
+}
+
+template <class Tr>
+void launch_gradient(const void* logits, int64_t N, int64_t V, int64_t row_stride, const int32_t* ids, int32_t K, float scale, const float* rest_max,
+                     const float* rest_coef, const float* top_grad, float grad_out, const float* grad_scale, void* dlogits, hipStream_t st)
+{
+    using elem = typename Tr::elem;
+    const int64_t all = (V + Tr::kPerVec - 1) / Tr::kPerVec;
+    hipLaunchKernelGGL((distill_dense_kernel<Tr>), rows_grid((unsigned)((all + kThreads - 1) / kThreads), N), dim3(kThreads), 0, st,
+                       (const elem*)logits, N, row_stride, (int32_t)V, scale, rest_max, rest_coef, grad_out, grad_scale, (elem*)dlogits);
+    hipLaunchKernelGGL((distill_top_kernel<Tr>), dim3((unsigned)((N * K + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, ids, top_grad, N,
+                       row_stride, (int32_t)V, K, grad_out, grad_scale, (elem*)dlogits);
+}
+
+int32_t launch_forward(const void* logits, int32_t dt, const Layout& l, const DistillArgs& a, hipStream_t st)
+{
+    hipLaunchKernelGGL(distill_target_kernel, dim3((unsigned)((a.N + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
+    const bool ok = dt == ULORL_BF16 ? launch_pieces<StoreBF16>(l, logits, a, st) : launch_pieces<StoreF32>(l, logits, a, st);
+    if (!ok) return ULORL_ERR_HIP;
+    const int64_t groups = (a.N + kWaves - 1) / kWaves;
+    hipLaunchKernelGGL(distill_finish_kernel, dim3((unsigned)(groups < kFinishGroups ? groups : kFinishGroups)), dim3(kThreads), 0, st, a);
+    return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
+}
+
+int32_t distill_args(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t& row_stride, const int32_t* teacher_ids, const float* teacher_logp,
+                     int32_t K, const float* weights, const ulorl_distill_params* p, float* loss, float* kl, float* lse, float* rest_max,
+                     float* rest_coef, float* top_grad, int64_t* counters, void* workspace, size_t workspace_bytes, Layout& l, DistillArgs& a)
+{
+    const int32_t rc = check_distill(logits, dt, N, V, row_stride, teacher_ids, K);
+    if (rc != ULORL_OK) return rc;
+    if (!teacher_logp || !p || !loss || !kl || !lse || !rest_max || !rest_coef || !top_grad) return ULORL_ERR_NULL;
+    if (!temperature_ok(p->temperature) || p->tail < ULORL_TAIL_BUCKET || p->tail > ULORL_TAIL_DROP || p->reserved[0] != 0 || p->reserved[1] != 0 ||
+        !(p->denominator == p->denominator))
+        return ULORL_ERR_PARAM;
+    l = layout_of(N, V, dt);
+    if (!workspace || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < l.total) return ULORL_ERR_WORKSPACE;
+    char* ws = (char*)workspace;
+    a.ids = teacher_ids; a.teacher = teacher_logp; a.weights = weights;
+    a.loss = loss; a.kl = kl; a.lse = lse; a.rest_max = rest_max; a.rest_coef = rest_coef; a.top_grad = top_grad; a.counters = counters;
+    a.target = (RowTarget*)(ws + l.target);
+    a.slots = (unsigned long long*)(ws + l.slots);
+    a.partial = (Partial*)(ws + l.partial);
+    a.ticket = (uint32_t*)(ws + l.ticket);
+    a.N = N; a.row_stride = row_stride; a.V = (int32_t)V; a.K = K; a.C = l.shape.pieces; a.tail = p->tail;
+    a.inv_t = 1.0 / (double)p->temperature;
+    a.scale = (float)(1.4426950408889634074 * a.inv_t);
+    a.inv_D = 1.0 / (p->denominator > 0.0 ? p->denominator : (double)N);
+    return ULORL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ulorl_distill_workspace_bytes(int64_t N, int64_t V, int32_t dt)
+{
+    if (!shape_ok(N, V, V) || N > kMaxDistillRows || (dt != ULORL_F32 && dt != ULORL_BF16)) return 0;
+    return layout_of(N, V, dt).total;
+}
+
+int32_t ulorl_distill_fwd(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t* teacher_ids,
+                          const float* teacher_logp, int32_t K, const float* weights, const ulorl_distill_params* p, float* loss, float* kl,
+                          float* lse, float* rest_max, float* rest_coef, float* top_grad, int64_t* counters, void* workspace,
+                          size_t workspace_bytes, void* hip_stream)
+{
+    Layout l;
+    DistillArgs a;
+    const int32_t rc = distill_args(logits, dt, N, V, row_stride, teacher_ids, teacher_logp, K, weights, p, loss, kl, lse, rest_max, rest_coef,
+                                    top_grad, counters, workspace, workspace_bytes, l, a);
+    if (rc != ULORL_OK) return rc;
+    return launch_forward(logits, dt, l, a, (hipStream_t)hip_stream);
+}
+
+int32_t ulorl_distill_bwd(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t* teacher_ids, int32_t K,
+                          float temperature, const float* rest_max, const float* rest_coef, const float* top_grad, float grad_out,
+                          const float* grad_scale, void* dlogits, void* hip_stream)
+{
+    const int32_t rc = check_distill(logits, dt, N, V, row_stride, teacher_ids, K);
+    if (rc != ULORL_OK) return rc;
+    if (!rest_max || !rest_coef || !top_grad || !dlogits) return ULORL_ERR_NULL;
+    if (((uintptr_t)dlogits & 15u) != 0) return ULORL_ERR_ALIGN;
+    if (!temperature_ok(temperature)) return ULORL_ERR_PARAM;
+    const float scale = (float)(1.4426950408889634074 / (double)temperature);
+    if (dt == ULORL_BF16)
+        launch_gradient<StoreBF16>(logits, N, V, row_stride, teacher_ids, K, scale, rest_max, rest_coef, top_grad, grad_out, grad_scale, dlogits,
+                                   (hipStream_t)hip_stream);
+    else
+        launch_gradient<StoreF32>(logits, N, V, row_stride, teacher_ids, K, scale, rest_max, rest_coef, top_grad, grad_out, grad_scale, dlogits,
+                                  (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
+}
+
+int32_t ulorl_distill_fwd_bwd(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t* teacher_ids,
+                              const float* teacher_logp, int32_t K, const float* weights, const ulorl_distill_params* p, float grad_out,
+                              float* loss, float* kl, float* lse, float* rest_max, float* rest_coef, float* top_grad, int64_t* counters,
+                              void* dlogits, void* workspace, size_t workspace_bytes, const ulorl_launch* launch, void* hip_stream)
+{
+    Layout l;
+    DistillArgs a;
+    int32_t rc = distill_args(logits, dt, N, V, row_stride, teacher_ids, teacher_logp, K, weights, p, loss, kl, lse, rest_max, rest_coef, top_grad,
+                              counters, workspace, workspace_bytes, l, a);
+    if (rc != ULORL_OK) return rc;
+    if (!dlogits) return ULORL_ERR_NULL;
+    if (((uintptr_t)dlogits & 15u) != 0) return ULORL_ERR_ALIGN;
+    LaunchOpts opts;
+    rc = resolve_launch(launch, &opts);
+    if (rc != ULORL_OK) return rc;
+    rc = launch_forward(logits, dt, l, a, (hipStream_t)hip_stream);
+    if (rc != ULORL_OK) return rc;
+    return ulorl_distill_bwd(logits, dt, N, V, row_stride, teacher_ids, K, p->temperature, rest_max, rest_coef, top_grad, grad_out, nullptr, dlogits,
+                             hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,112 @@
+// Sums over a row's softmax as a lane forms them, under a temperature and with masked logits: shared by the kernels behind
+// ulorl_token_topk and ulorl_distill_*.
+#ifndef ULORL_ROW_SUMS_HPP
+#define ULORL_ROW_SUMS_HPP
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "logits_stream.hpp"
+
+namespace ulorl_detail {
+
+// Logits at or below -9e29 are masked (the filler of short vectors is one of them).  A lane's running maximum starts a little
+// above: by so much that the terms of masked logits are 0 against it (the rounding of m scale is 1e23 there).
+constexpr float kFloor = -8.99e29f;
+
+// Per-lane statistics of the stream; x = z scale in log2 units, relative to the lane's maximum.
+// S + Sc: sum 2^(x - mL), its rounding residuals carried in Sc; T: sum 2^(x - mL) (x - mL).
+struct Lane {
+    float m, mL, S, Sc, T;
+};
+
+// The larger, not-a-number if one is (a row that holds one is refused at its end): one instruction for three values, and none to
+// quiet what came out of bit operations, which fmaxf needs.
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
+// WEIGHTED: T is wanted.
+template <int COUNT, bool WEIGHTED = true>
+__device__ __forceinline__ void absorb_scaled(const float* f, float cm, float scale, Lane& a)
+{
+    const float mn = larger(a.m, cm);
+    const float mLn = mn * scale;
+    const float d = a.mL - mLn;
+    const float sc = fast_exp2(d);
+    float T = WEIGHTED ? sc * fmaf(d, a.S, a.T) : 0.0f;
+    const float S = sc * a.S, Sc = sc * a.Sc;
+    // the terms as a tree over neighbours: a sum of eight is done before the next eight terms are formed
+    float e[COUNT / 8 > 0 ? COUNT / 8 : 1];
+#pragma unroll
+    for (int c = 0; c < COUNT; c += 8) {
+        constexpr int W = COUNT < 8 ? COUNT : 8;
+        float p[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const float x = fmaf(f[c + k], scale, -mLn);
+            p[k] = fast_exp2(x);
+            if constexpr (WEIGHTED) T = fmaf(p[k], x, T);
+        }
+#pragma unroll
+        for (int w = W / 2; w >= 1; w >>= 1)
+#pragma unroll
+            for (int k = 0; k < w; ++k) p[k] += p[k + w];
+        e[c / 8] = p[0];
+    }
+#pragma unroll
+    for (int w = COUNT / 16; w >= 1; w >>= 1)
+#pragma unroll
+        for (int k = 0; k < w; ++k) e[k] += e[k + w];
+    const float t = S + e[0];                   // TwoSum: the residual of a small term against a sum near 1 is kept
+    const float bv = t - S;
+    a.Sc = Sc + ((S - (t - bv)) + (e[0] - bv));
+    a.S = t;
+    a.T = T;
+    a.m = mn;
+    a.mL = mLn;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x)
+{
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140, kRotate8 = 0x128;      // 7 - lane in each 8, 15 - lane in each 16
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = larger(x, from_lane<kXor1>(x));
+    x = larger(x, from_lane<kXor2>(x));
+    x = larger(x, from_lane<kMirror8>(x));
+    x = larger(x, from_lane<kMirror16>(x));
+    const int i = __float_as_int(x);
+    return larger(larger(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
+                  larger(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
+}
+
+// A vector of a row; behind the row's end, and where V ends inside a vector, the filler.
+template <class Tr>
+__device__ __forceinline__ u32x4 load_vector(const typename Tr::elem* rowp, int32_t V, int i)
+{
+    constexpr int E = Tr::kPerVec;
+    const int nvec = V / E;
+    if (i < nvec) return load_stream(reinterpret_cast<const u32x4*>(rowp) + i);
+    u32x4 v = Tr::filler();
+    if (i == nvec) {
+        for (int e = 0; e < V - nvec * E; ++e) {
+            if constexpr (E == 8) {
+                const uint32_t b = rowp[i * E + e];
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    if (w == (e >> 1)) v[w] = (e & 1) ? (v[w] & 0xffffu) | (b << 16) : (v[w] & 0xffff0000u) | b;
+            } else {
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    if (w == e) v[w] = __float_as_uint(rowp[i * E + e]);
+            }
+        }
+    }
+    return v;
+}
+
+}  // namespace ulorl_detail
+
+#endif

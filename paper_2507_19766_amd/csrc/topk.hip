@@ -24,6 +24,7 @@
 #include <type_traits>
 
 #include "logits_stream.hpp"
+#include "row_sums.hpp"
 #include "ulorl.h"
 #include "ulorl_internal.hpp"
 
@@ -49,9 +50,6 @@ constexpr int kMaxPieces = 64;
 constexpr int64_t kSplitRows = 160;
 constexpr int64_t kSplitBatches = 8;          // of 16 KB
 constexpr int64_t kFewWorkgroups = 1024;
-// Logits at or below -9e29 are masked (the filler of short vectors is one of them).  A lane's running maximum starts a little
-// above: by so much that the terms of masked logits are 0 against it (the rounding of m scale is 1e23 there).
-constexpr float kFloor = -8.99e29f;
 
 struct TopkArgs {
     const int32_t* token_ids;   // may be NULL
@@ -67,56 +65,6 @@ struct TopkArgs {
     float scale;                // log2(e) / T
     double inv_t;
 };
-
-// Per-lane statistics of the stream; x = z scale in log2 units, relative to the lane's maximum.
-// S + Sc: sum 2^(x - mL), its rounding residuals carried in Sc; T: sum 2^(x - mL) (x - mL).
-struct Lane {
-    float m, mL, S, Sc, T;
-};
-
-// The larger, not-a-number if one is (a row that holds one is refused at its end): one instruction for three values, and none to
-// quiet what came out of bit operations, which fmaxf needs.
-__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
-
-template <int COUNT>
-__device__ __forceinline__ void absorb_scaled(const float* f, float cm, float scale, Lane& a)
-{
-    const float mn = larger(a.m, cm);
-    const float mLn = mn * scale;
-    const float d = a.mL - mLn;
-    const float sc = fast_exp2(d);
-    float T = sc * fmaf(d, a.S, a.T);
-    const float S = sc * a.S, Sc = sc * a.Sc;
-    // the terms as a tree over neighbours: a sum of eight is done before the next eight terms are formed
-    float e[COUNT / 8 > 0 ? COUNT / 8 : 1];
-#pragma unroll
-    for (int c = 0; c < COUNT; c += 8) {
-        constexpr int W = COUNT < 8 ? COUNT : 8;
-        float p[W];
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-            const float x = fmaf(f[c + k], scale, -mLn);
-            p[k] = fast_exp2(x);
-            T = fmaf(p[k], x, T);
-        }
-#pragma unroll
-        for (int w = W / 2; w >= 1; w >>= 1)
-#pragma unroll
-            for (int k = 0; k < w; ++k) p[k] += p[k + w];
-        e[c / 8] = p[0];
-    }
-#pragma unroll
-    for (int w = COUNT / 16; w >= 1; w >>= 1)
-#pragma unroll
-        for (int k = 0; k < w; ++k) e[k] += e[k + w];
-    const float t = S + e[0];                   // TwoSum: the residual of a small term against a sum near 1 is kept
-    const float bv = t - S;
-    a.Sc = Sc + ((S - (t - bv)) + (e[0] - bv));
-    a.S = t;
-    a.T = T;
-    a.m = mn;
-    a.mL = mLn;
-}
 
 // Absorbs U vectors and gives each one's largest element.
 template <class Tr, int U>
@@ -153,12 +101,6 @@ __device__ __forceinline__ void absorb_vectors(const u32x4 (&v)[U], float scale,
     }
 }
 
-template <int CTRL>
-__device__ __forceinline__ float from_lane(float x)
-{
-    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
-}
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140, kRotate8 = 0x128;      // 7 - lane in each 8, 15 - lane in each 16
 // Of two vectors' maxima a lane keeps the one that its bit says, with what its partner has of it.
 template <int CTRL>
 __device__ __forceinline__ float keep_one(float lo, float hi, bool bit)
@@ -188,17 +130,6 @@ __device__ __forceinline__ int kept_vector(int lane)
 {
     return LG == 2 ? (lane & 3) : ((lane >> 1) & 3);
 }
-__device__ __forceinline__ float wave_max(float x)
-{
-    x = larger(x, from_lane<kXor1>(x));
-    x = larger(x, from_lane<kXor2>(x));
-    x = larger(x, from_lane<kMirror8>(x));
-    x = larger(x, from_lane<kMirror16>(x));
-    const int i = __float_as_int(x);
-    return larger(larger(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
-                  larger(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
-}
-
 // Order-preserving bits of a logit, -0 as +0; 0: masked.
 __device__ __forceinline__ uint32_t key_of(float f)
 {
@@ -260,31 +191,6 @@ __device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared& s
         r.T += sw * (sh.T[w] + (double)dw * sh.S[w]);
     }
     return r;
-}
-
-// A vector of a row; behind the row's end, and where V ends inside a vector, the filler.
-template <class Tr>
-__device__ __forceinline__ u32x4 load_vector(const typename Tr::elem* rowp, int32_t V, int i)
-{
-    constexpr int E = Tr::kPerVec;
-    const int nvec = V / E;
-    if (i < nvec) return load_stream(reinterpret_cast<const u32x4*>(rowp) + i);
-    u32x4 v = Tr::filler();
-    if (i == nvec) {
-        for (int e = 0; e < V - nvec * E; ++e) {
-            if constexpr (E == 8) {
-                const uint32_t b = rowp[i * E + e];
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    if (w == (e >> 1)) v[w] = (e & 1) ? (v[w] & 0xffffu) | (b << 16) : (v[w] & 0xffff0000u) | b;
-            } else {
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    if (w == e) v[w] = __float_as_uint(rowp[i * E + e]);
-            }
-        }
-    }
-    return v;
 }
 
 // Number of threads' items that hold, over the workgroup (uniform).  turn alternates, so that one barrier a call is enough.

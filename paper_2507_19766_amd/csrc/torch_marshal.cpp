@@ -61,7 +61,7 @@ void check(int32_t rc, const char* where)
 
 const char* type_name(at::ScalarType t)
 {
-    return t == at::kFloat ? "torch.float32" : t == at::kInt ? "torch.int32" : "torch.uint8";
+    return t == at::kFloat ? "torch.float32" : t == at::kInt ? "torch.int32" : t == at::kLong ? "torch.int64" : "torch.uint8";
 }
 
 // A contiguous vector of n elements on the device, or nothing.
@@ -324,6 +324,98 @@ TopFields token_topk(const Tensor& z, int64_t K, const OptTensor& token_ids, dou
     return f;
 }
 
+// The fields of DistillResult, in its order; a caller's are written or refused.
+enum { DIS_LOSS, DIS_KL, DIS_LSE, DIS_REST_MAX, DIS_REST_COEF, DIS_TOP_GRAD, DIS_COUNTERS, DIS_FIELDS };
+using DistillFields = std::array<Tensor, DIS_FIELDS>;
+
+struct Teacher {
+    Tensor ids, logp;
+    OptTensor weights;
+    const ulorl_distill_params* params;
+    int64_t K = 0;
+
+    void check(int64_t N, const at::Device& dev)
+    {
+        TORCH_CHECK_VALUE(ids.dim() == 2, "teacher_ids must be [N, K]");
+        K = ids.size(1);
+        check_matrix(ids, at::kInt, N, K, "teacher_ids", dev);
+        check_matrix(logp, at::kFloat, N, K, "teacher_logp", dev);
+        check_vector(weights, at::kFloat, N, "weights", dev);
+        TORCH_CHECK_VALUE(K >= 1 && K <= 128, "teacher_ids must list 1 to 128 tokens a row, got ", K);
+    }
+};
+
+void distill_fields(DistillFields& f, const std::optional<std::vector<OptTensor>>& out, int64_t N, int64_t K, const at::Device& dev)
+{
+    if (!out.has_value()) {
+        f[DIS_LOSS] = empty(1, at::kFloat, dev);
+        for (int i : {DIS_KL, DIS_LSE, DIS_REST_MAX, DIS_REST_COEF}) f[i] = empty(N, at::kFloat, dev);
+        f[DIS_TOP_GRAD] = empty_matrix(N, K, at::kFloat, dev);
+        f[DIS_COUNTERS] = empty(4, at::kLong, dev);
+        return;
+    }
+    static const char* const names[] = {"out.loss", "out.kl", "out.lse", "out.rest_max", "out.rest_coef", "out.top_grad", "out.counters"};
+    for (int i = 0; i < DIS_FIELDS; ++i) {
+        TORCH_CHECK_VALUE((*out)[i].has_value(), names[i], " is missing");
+        f[i] = *(*out)[i];
+    }
+    check_vector(f[DIS_LOSS], at::kFloat, 1, names[DIS_LOSS], dev);
+    for (int i : {DIS_KL, DIS_LSE, DIS_REST_MAX, DIS_REST_COEF}) check_vector(f[i], at::kFloat, N, names[i], dev);
+    check_matrix(f[DIS_TOP_GRAD], at::kFloat, N, K, names[DIS_TOP_GRAD], dev);
+    check_vector(f[DIS_COUNTERS], at::kLong, 4, names[DIS_COUNTERS], dev);
+}
+
+void distill_fwd(const Tensor& z, Teacher t, const std::optional<std::vector<OptTensor>>& out, const OptTensor& workspace, DistillFields& f)
+{
+    const Logits l = check_logits(z);
+    const c10::DeviceGuard guard(l.dev);
+    t.check(l.N, l.dev);
+    distill_fields(f, out, l.N, t.K, l.dev);
+    const Tensor ws = checked_workspace(workspace, ulorl_distill_workspace_bytes(l.N, l.V, l.dt), l.dev);
+    check(ulorl_distill_fwd(ptr(z), l.dt, l.N, l.V, l.stride, as<int32_t>(t.ids), as<float>(t.logp), (int32_t)t.K, as<float>(t.weights), t.params,
+                            as<float>(f[DIS_LOSS]), as<float>(f[DIS_KL]), as<float>(f[DIS_LSE]), as<float>(f[DIS_REST_MAX]),
+                            as<float>(f[DIS_REST_COEF]), as<float>(f[DIS_TOP_GRAD]), as<int64_t>(f[DIS_COUNTERS]), ptr(ws), ws.nbytes(),
+                            stream_of(l.dev)),
+          "ulorl_distill_fwd");
+}
+
+Tensor distill_fwd_bwd(const Tensor& z, Teacher t, double grad_out, const OptTensor& dlogits, bool inplace,
+                       const std::optional<std::vector<OptTensor>>& out, const OptTensor& workspace, const ulorl_launch* launch, DistillFields& f)
+{
+    const Logits l = check_logits(z);
+    const c10::DeviceGuard guard(l.dev);
+    t.check(l.N, l.dev);
+    distill_fields(f, out, l.N, t.K, l.dev);
+    const Tensor d = gradient_for(z, dlogits, inplace);
+    const Tensor ws = checked_workspace(workspace, ulorl_distill_workspace_bytes(l.N, l.V, l.dt), l.dev);
+    check(ulorl_distill_fwd_bwd(ptr(z), l.dt, l.N, l.V, l.stride, as<int32_t>(t.ids), as<float>(t.logp), (int32_t)t.K, as<float>(t.weights),
+                                t.params, (float)grad_out, as<float>(f[DIS_LOSS]), as<float>(f[DIS_KL]), as<float>(f[DIS_LSE]),
+                                as<float>(f[DIS_REST_MAX]), as<float>(f[DIS_REST_COEF]), as<float>(f[DIS_TOP_GRAD]),
+                                as<int64_t>(f[DIS_COUNTERS]), ptr(d), ptr(ws), ws.nbytes(), launch, stream_of(l.dev)),
+          "ulorl_distill_fwd_bwd");
+    return d;
+}
+
+Tensor distill_bwd(const Tensor& z, const Tensor& ids, const Tensor& rest_max, const Tensor& rest_coef, const Tensor& top_grad, double temperature,
+                   double grad_out, const OptTensor& grad_scale, const OptTensor& dlogits, bool inplace)
+{
+    const Logits l = check_logits(z);
+    const c10::DeviceGuard guard(l.dev);
+    TORCH_CHECK_VALUE(ids.dim() == 2, "teacher_ids must be [N, K]");
+    check_matrix(ids, at::kInt, l.N, ids.size(1), "teacher_ids", l.dev);
+    check_vector(rest_max, at::kFloat, l.N, "rest_max", l.dev);
+    check_vector(rest_coef, at::kFloat, l.N, "rest_coef", l.dev);
+    check_matrix(top_grad, at::kFloat, l.N, ids.size(1), "top_grad", l.dev);
+    if (grad_scale.has_value())
+        TORCH_CHECK_VALUE(grad_scale->device() == l.dev && grad_scale->scalar_type() == at::kFloat && grad_scale->numel() == 1,
+                          "grad_scale must be one float32 on ", l.dev.str());
+    const Tensor d = gradient_for(z, dlogits, inplace);
+    check(ulorl_distill_bwd(ptr(z), l.dt, l.N, l.V, l.stride, as<int32_t>(ids), (int32_t)ids.size(1), (float)temperature, as<float>(rest_max),
+                            as<float>(rest_coef), as<float>(top_grad), (float)grad_out, as<float>(grad_scale), ptr(d), stream_of(l.dev)),
+          "ulorl_distill_bwd");
+    return d;
+}
+
 struct Lmhead {
     int64_t N, Hd, V;
     at::Device dev;
@@ -396,6 +488,23 @@ struct TokenLossNode : torch::autograd::Function<TokenLossNode> {
     {
         const variable_list s = ctx->get_saved_variables();
         return {token_loss_bwd(s[0], s[1], s[2], s[3] * grad[0], 1.0, std::nullopt, false), Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+// The upstream gradient goes to the kernels as the device scalar that it is.
+struct DistillNode : torch::autograd::Function<DistillNode> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& logits, const Teacher* t, DistillFields* f)
+    {
+        distill_fwd(logits, *t, std::nullopt, std::nullopt, *f);
+        ctx->save_for_backward({logits, t->ids, (*f)[DIS_REST_MAX], (*f)[DIS_REST_COEF], (*f)[DIS_TOP_GRAD]});
+        ctx->saved_data["temperature"] = (double)t->params->temperature;
+        return (*f)[DIS_LOSS].reshape({});
+    }
+    static variable_list backward(AutogradContext* ctx, const variable_list& grad)
+    {
+        const variable_list s = ctx->get_saved_variables();
+        return {distill_bwd(s[0], s[1], s[2], s[3], s[4], ctx->saved_data["temperature"].toDouble(), 1.0, grad[0], std::nullopt, false), Tensor(),
+                Tensor()};
     }
 };
 
@@ -503,6 +612,31 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
                                bool inplace) { return unlocked([&] { return token_loss_bwd(z, y, lse, g, grad_out, d, inplace); }); });
     m.def("token_topk", [](const Tensor& z, int64_t K, const OptTensor& y, double temperature, const Given& out, const OptTensor& ws) {
         return list_of(unlocked([&] { return token_topk(z, K, y, temperature, out, ws); }));
+    });
+    m.def("distill_fwd", [](const Tensor& z, const Tensor& ids, const Tensor& logp, const OptTensor& weights, uintptr_t params, const Given& out,
+                            const OptTensor& ws) {
+        DistillFields f;
+        unlocked([&] { distill_fwd(z, Teacher{ids, logp, weights, reinterpret_cast<const ulorl_distill_params*>(params)}, out, ws, f); });
+        return list_of(f);
+    });
+    m.def("distill_fwd_bwd", [](const Tensor& z, const Tensor& ids, const Tensor& logp, const OptTensor& weights, uintptr_t params, double grad_out,
+                                const OptTensor& d, bool inplace, const Given& out, const OptTensor& ws, uintptr_t launch) {
+        DistillFields f;
+        const Tensor dz = unlocked([&] {
+            return distill_fwd_bwd(z, Teacher{ids, logp, weights, reinterpret_cast<const ulorl_distill_params*>(params)}, grad_out, d, inplace, out,
+                                   ws, reinterpret_cast<const ulorl_launch*>(launch), f);
+        });
+        return py::make_tuple(list_of(f), dz);
+    });
+    m.def("distill_bwd", [](const Tensor& z, const Tensor& ids, const Tensor& rest_max, const Tensor& rest_coef, const Tensor& top_grad,
+                            double temperature, double grad_out, const OptTensor& grad_scale, const OptTensor& d, bool inplace) {
+        return unlocked([&] { return distill_bwd(z, ids, rest_max, rest_coef, top_grad, temperature, grad_out, grad_scale, d, inplace); });
+    });
+    m.def("autograd_distill", [](const Tensor& z, const Tensor& ids, const Tensor& logp, const OptTensor& weights, uintptr_t params, bool want_fields) {
+        const Teacher t{ids, logp, weights, reinterpret_cast<const ulorl_distill_params*>(params)};
+        DistillFields f;
+        const Tensor loss = unlocked([&] { return DistillNode::apply(z, &t, &f); });
+        return py::make_tuple(loss, want_fields ? list_of(f) : py::list());
     });
     m.def("lmhead_fwd", [](const Tensor& h, const Tensor& w, OptTensor y, OptTensor cu, OptTensor adv, OptTensor old, OptTensor ids,
                            uintptr_t params, uintptr_t launch, int64_t chunk, const Given& out, const OptTensor& ws, int64_t K) {
