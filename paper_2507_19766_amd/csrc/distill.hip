@@ -12,6 +12,7 @@
 //
 //   distill_target_kernel   one wave per row: is the target a distribution; what the row's gradient needs of it
 //   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers, to (max, S); listed logits
+//   distill_row_kernel      one call: the same pieces, which tell each other their sums and write the gradient from the registers
 //   distill_finish_kernel   one wave per row: kl, the listed tokens' gradients, the unlisted ones' coefficient; the loss
 //   distill_dense_kernel    the gradient of all tokens as if unlisted, one 16-byte vector per thread
 //   distill_top_kernel      the listed tokens' gradients over it
@@ -63,8 +64,11 @@ struct DistillArgs {
     int64_t* counters;          // may be NULL
     RowTarget* target;          // [N]
     unsigned long long* slots;  // [N * C * 2]: {max, S} of a piece's unlisted logits, {max, S} of its listed ones
+    unsigned long long* pending;    // [N], one call: pieces whose gradient is not written, because a wait expired
     Partial* partial;           // [kFinishGroups]
-    uint32_t* ticket;
+    uint32_t* flags;            // ticket of the finishing kernel; one call: whether any wait expired
+    int32_t spin_limit;         // one call: polls before a wait is given up; 0: two passes
+    float grad_out;
     int64_t N, row_stride;
     int32_t V, K, C;
     int32_t tail;
@@ -84,8 +88,15 @@ __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
 {
     const int lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0u;
+    if (blockIdx.x == 0 && threadIdx.x < 2) a.flags[threadIdx.x] = 0u;
     if (row >= a.N) return;
+    if (a.spin_limit > 0) {         // the exchange of the one-call path starts from zeros
+        if (lane == 0) a.pending[row] = 0ull;
+        if (a.C > 1 && lane < a.C) {
+            a.slots[(row * a.C + lane) * 2] = 0ull;
+            a.slots[(row * a.C + lane) * 2 + 1] = 0ull;
+        }
+    }
     const float w = a.weights ? a.weights[row] : 1.0f;
     int32_t id[2];
     float l[2];
@@ -282,10 +293,132 @@ __global__ __launch_bounds__(kThreads) void distill_piece_kernel(const typename 
     }
 }
 
+// The gradient of a vector's tokens as if unlisted: c e^((z - m) / T).
+// In bf16 c e^(x - m) = sign(c) 2^(z scale + log2|c| - m scale), one fused step and one exp2; in fp32, where the rounding of that sum
+// (|m scale| and |log2 c| are tens) would be ten units of the result, c 2^((z - m) scale).
+struct RestGradient {
+    float c, m, shift, scale;
+    bool none;                  // zeros: no coefficient, or one that is no number
+    __device__ __forceinline__ RestGradient(float coef, float max, float scale_) : c(coef), m(max), scale(scale_)
+    {
+        none = c == 0.0f || !finite(c);
+        shift = none ? 0.0f : fmaf(-m, scale, log2f(fabsf(c)));
+    }
+    template <class Tr>
+    __device__ __forceinline__ u32x4 of(const u32x4& v) const
+    {
+        constexpr int E = Tr::kPerVec;
+        float f[E];
+        Tr::unpack(v, f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = E == 4 ? c * fast_exp2((f[e] - m) * scale) : fast_exp2(fmaf(f[e], scale, shift));
+        u32x4 o = Tr::pack(f);
+        if (E == 8 && c < 0.0f) o ^= Tr::sign_bits();
+        return o;
+    }
+};
+
+// Stores vector i of a row's gradient; where V ends inside it, the elements that there are.
+template <class Tr>
+__device__ __forceinline__ void store_vector(typename Tr::elem* outp, int32_t V, int i, const u32x4& o)
+{
+    constexpr int E = Tr::kPerVec;
+    const int nvec = V / E;
+    if (i < nvec) {
+        store_stream(reinterpret_cast<u32x4*>(outp) + i, o);
+    } else if (i == nvec) {
+        float f[E];
+        Tr::unpack(o, f);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < V - nvec * E) Tr::store1(outp + i * E + e, f[e]);
+    }
+}
+
+// One call: the pieces of a row keep their logits in registers, tell each other their sums and write the gradient of their
+// unlisted tokens; every logit is read once and every gradient written once (the listed tokens' over it, by
+// distill_top_kernel).  A piece's two words in a.slots, zero before, are relaxed agent-scope atomics that carry their own validity.
+// A row's pieces are neighbours in dispatch order, so partners are resident or next in line; the wait is bounded all the same: a
+// workgroup whose wait expires writes nothing (in place, its logits stay) and marks its piece, which distill_finish_kernel then
+// writes.
+template <class Tr, int VPT>
+__global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, DistillArgs a)
+{
+    constexpr int NT = kThreads;
+    __shared__ PieceShared sh;
+    __shared__ float bc_coef, bc_max;
+    __shared__ int bc_expired;
+    const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
+    if (row >= a.N) return;
+    const int tid = threadIdx.x, c = (int)blockIdx.x, first = c * NT * VPT;
+    const int nvec = a.V / Tr::kPerVec;
+    typename Tr::elem* outp = dlogits + row * a.row_stride;
+    char* const piece_out = reinterpret_cast<char*>(outp) + ((size_t)first << 4);
+    const bool full = first + NT * VPT <= nvec;
+    const RowTarget target = a.target[row];
+    u32x4 v[VPT];
+    auto store_all = [&](const auto& value) {
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+            if (full) store_stream(reinterpret_cast<u32x4*>(piece_out + (size_t)k * NT * 16 + ((uint32_t)tid << 4)), value(k));
+            else store_vector<Tr>(outp, a.V, first + k * NT + tid, value(k));
+        }
+    };
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    if (target.state != ROW_ON) {
+        store_all([&](int) { return zero; });
+        return;
+    }
+    const PieceSums p = piece_sums<Tr, VPT>(a, logits + row * a.row_stride, row, c, v, sh);
+    if (tid < 64) {
+        unsigned long long* slot = a.slots + row * a.C * 2;
+        unsigned long long w0 = slot_word(p.m, p.S), w1 = slot_word(p.top_m, p.top_S);
+        bool expired = false;
+        if (tid == 0) {
+            __hip_atomic_store(slot + 2 * c, w0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(slot + 2 * c + 1, w1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        if (a.C > 1) {
+            w0 = w1 = 0;
+            for (int spins = 0; tid < a.C;) {
+                if (w0 == 0) w0 = __hip_atomic_load(slot + 2 * tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (w1 == 0) w1 = __hip_atomic_load(slot + 2 * tid + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (w0 != 0 && w1 != 0) break;
+                if (++spins >= a.spin_limit) { expired = true; break; }
+                __builtin_amdgcn_s_sleep(4);
+            }
+            expired = __any(expired);
+        }
+        const bool mine = tid < a.C;
+        const float m = mine ? __uint_as_float((uint32_t)w0) : kFloor, tm = mine ? __uint_as_float((uint32_t)w1) : kFloor;
+        const double S = mine ? (double)__uint_as_float((uint32_t)(w0 >> 32)) : 0.0, tS = mine ? (double)__uint_as_float((uint32_t)(w1 >> 32)) : 0.0;
+        const float rest_max = wave_max(m), M = larger(rest_max, wave_max(tm));
+        const double rest = wave_sum_f64((double)fast_exp2((m - rest_max) * a.scale) * S);      // relative to rest_max
+        const double top = wave_sum_f64((double)fast_exp2((tm - M) * a.scale) * tS);            // relative to M
+        const double R = (double)fast_exp2((rest_max - M) * a.scale) * rest;
+        if (tid == 0) {
+            bc_coef = rest != 0.0 ? (float)(((double)target.mass * (R / (R + top)) - (double)target.rest) / rest) * a.grad_out : 0.0f;
+            bc_max = rest_max;
+            bc_expired = expired;
+            if (expired) {
+                __hip_atomic_fetch_or(a.pending + row, 1ull << c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                a.flags[1] = 1u;
+            }
+        }
+    }
+    __syncthreads();
+    if (bc_expired) return;
+    const RestGradient grad(bc_coef, bc_max, a.scale);
+    if (grad.none) store_all([&](int) { return zero; });
+    else store_all([&](int k) { return grad.template of<Tr>(v[k]); });
+}
+
 // ---------------------------------------------------------------------------------------------
 // the rows' results
 // ---------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a)
+template <class Tr>
+__global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, int32_t piece_vectors,
+                                                                  DistillArgs a)
 {
     __shared__ Partial part[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -382,6 +515,19 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a)
             a.rest_coef[row] = coef_out;
         }
     }
+    if (a.spin_limit > 0 && a.flags[1] != 0u) {     // pieces whose workgroup waited in vain: their logits are whole, in place too
+        __threadfence();                            // the rows' results are this wave's own
+        const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
+        for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.N; row += (int64_t)gridDim.x * kWaves) {
+            for (unsigned long long todo = a.pending[row]; todo != 0ull; todo &= todo - 1ull) {
+                const RestGradient rest(a.rest_coef[row] * a.grad_out, a.rest_max[row], a.scale);
+                const int begin = (__ffsll((long long)todo) - 1) * piece_vectors;
+                for (int i = begin + lane; i < min(all, begin + piece_vectors); i += 64)
+                    store_vector<Tr>(dlogits + row * a.row_stride, a.V, i,
+                                     rest.none ? u32x4{0u, 0u, 0u, 0u} : rest.template of<Tr>(load_vector<Tr>(logits + row * a.row_stride, a.V, i)));
+            }
+        }
+    }
     if (lane == 0) part[wave] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -401,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a)
         publish(&to.empty, sum.empty);
         publish(&to.status, sum.status);
     }
-    if (!last_workgroup(a.ticket, gridDim.x)) return;
+    if (!last_workgroup(a.flags, gridDim.x)) return;
     // all sums in a fixed order: lanes over workgroups, then lanes, then waves
     Partial q = {0.0, 0, 0, 0, 0};
     for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads) {
@@ -445,45 +591,20 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a)
 // ---------------------------------------------------------------------------------------------
 // the gradient
 // ---------------------------------------------------------------------------------------------
-// A coefficient that leaves a row zeros: none, or one that is no number.
-__device__ __forceinline__ bool no_gradient(float c) { return c == 0.0f || !finite(c); }
-
 // rest_coef e^((z - rest_max) / T) of every token: 4 KB of one row per workgroup, the shape in which a read-and-write stream is
-// fastest here.  In bf16 c e^(x - m) = sign(c) 2^(z scale + log2|c| - m scale), one fused step and one exp2; in fp32, where the
-// rounding of that sum (|m scale| and |log2 c| are tens) would be ten units of the result, c 2^((z - m) scale).
+// fastest here.
 template <class Tr>
 __global__ __launch_bounds__(kThreads) void distill_dense_kernel(const typename Tr::elem* logits, int64_t N, int64_t row_stride, int32_t V, float scale,
                                                                  const float* rest_max, const float* rest_coef, float grad_out,
                                                                  const float* grad_scale, typename Tr::elem* dlogits)
 {
-    constexpr int E = Tr::kPerVec;
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
     if (row >= N) return;
-    const float c = rest_coef[row] * (grad_scale ? *grad_scale * grad_out : grad_out);
-    const typename Tr::elem* rowp = logits + row * row_stride;
-    typename Tr::elem* outp = dlogits + row * row_stride;
-    const int nvec = V / E, i = (int)blockIdx.x * kThreads + (int)threadIdx.x;
-    const bool none = no_gradient(c);
-    constexpr bool EXACT = E == 4;
-    const float m = rest_max[row], shift = none || EXACT ? 0.0f : fmaf(-m, scale, log2f(fabsf(c)));
-    if (i < nvec) {
-        u32x4 o = {0u, 0u, 0u, 0u};
-        if (!none) {
-            float f[E];
-            Tr::unpack(load_stream(reinterpret_cast<const u32x4*>(rowp) + i), f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = EXACT ? c * fast_exp2((f[e] - m) * scale) : fast_exp2(fmaf(f[e], scale, shift));
-            o = Tr::pack(f);
-            if (!EXACT && c < 0.0f) o ^= Tr::sign_bits();
-        }
-        store_stream(reinterpret_cast<u32x4*>(outp) + i, o);
-    } else if (i == nvec) {
-        for (int j = nvec * E; j < V; ++j) {
-            float x = 0.0f;
-            if (!none) x = EXACT ? fabsf(c) * fast_exp2((Tr::load1(rowp + j) - m) * scale) : fast_exp2(fmaf(Tr::load1(rowp + j), scale, shift));
-            Tr::store1(outp + j, c < 0.0f ? -x : x);
-        }
-    }
+    const RestGradient grad(rest_coef[row] * (grad_scale ? *grad_scale * grad_out : grad_out), rest_max[row], scale);
+    const int i = (int)blockIdx.x * kThreads + (int)threadIdx.x;
+    u32x4 o = {0u, 0u, 0u, 0u};
+    if (!grad.none) o = grad.template of<Tr>(load_vector<Tr>(logits + row * row_stride, V, i));
+    store_vector<Tr>(dlogits + row * row_stride, V, i, o);
 }
 
 template <class Tr>
@@ -502,8 +623,9 @@ __global__ __launch_bounds__(kThreads) void distill_top_kernel(const int32_t* id
 // host side
 // ---------------------------------------------------------------------------------------------
 struct Layout {
-    size_t target, partial, ticket, slots, total;
+    size_t target, partial, flags, pending, slots, total;
     ClusterShape shape;         // vectors per thread, pieces per row
+    bool cooperative;           // a wave can poll a row's pieces
 };
 
 Layout layout_of(int64_t N, int64_t V, int32_t dt)
@@ -511,15 +633,17 @@ Layout layout_of(int64_t N, int64_t V, int32_t dt)
     Layout l;
     const int64_t E = dt == ULORL_F32 ? 4 : 8, all = (V + E - 1) / E;
     l.shape = cluster_shape(all * E, dt);
+    l.cooperative = l.shape.pieces > 0;
     if (l.shape.pieces == 0) {                      // more than 64 pieces: no limit to the two-pass path
         l.shape.vpt = 15;
         l.shape.pieces = (int)((all + kThreads * 15 - 1) / (kThreads * 15));
     }
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     size_t off = 0;
-    l.ticket = off;  off += 256;
+    l.flags = off;   off += 256;
     l.partial = off; off = up(off + sizeof(Partial) * kFinishGroups);
     l.target = off;  off = up(off + sizeof(RowTarget) * (size_t)N);
+    l.pending = off; off = up(off + sizeof(unsigned long long) * (size_t)N);
     l.slots = off;   off = up(off + 16 * (size_t)N * (size_t)l.shape.pieces);
     l.total = off;
     return l;
@@ -536,14 +660,20 @@ int32_t check_distill(const void* logits, int32_t dt, int64_t N, int64_t V, int6
     return ids ? ULORL_OK : ULORL_ERR_NULL;
 }
 
+// The stream over the logits: with dlogits and a spin limit the one-call kernel, else the sums alone.
 template <class Tr>
-bool launch_pieces(const Layout& l, const void* logits, const DistillArgs& a, hipStream_t st)
+bool launch_stream(const Layout& l, const void* logits, void* dlogits, const DistillArgs& a, hipStream_t st)
 {
+    using elem = typename Tr::elem;
+    // x: piece (fastest, so a row's pieces have consecutive linear ids), y/z: row
     const dim3 grid = rows_grid((unsigned)a.C, a.N);
-#define ULORL_CASE(VPT_)                                                                                                          \
-    if (l.shape.vpt == VPT_) {                                                                                                    \
-        hipLaunchKernelGGL((distill_piece_kernel<Tr, VPT_>), grid, dim3(kThreads), 0, st, (const typename Tr::elem*)logits, a);   \
-        return true;                                                                                                              \
+#define ULORL_CASE(VPT_)                                                                                                                   \
+    if (l.shape.vpt == VPT_) {                                                                                                             \
+        if (a.spin_limit > 0)                                                                                                              \
+            hipLaunchKernelGGL((distill_row_kernel<Tr, VPT_>), grid, dim3(kThreads), 0, st, (const elem*)logits, (elem*)dlogits, a);       \
+        else                                                                                                                               \
+            hipLaunchKernelGGL((distill_piece_kernel<Tr, VPT_>), grid, dim3(kThreads), 0, st, (const elem*)logits, a);                     \
+        return true;                                                                                                                       \
     }
     ULORL_CASE(4) ULORL_CASE(8) ULORL_CASE(13) ULORL_CASE(15)
     if constexpr (Tr::kPerVec == 8) {
@@ -556,24 +686,38 @@ bool launch_pieces(const Layout& l, const void* logits, const DistillArgs& a, hi
 }
 
 template <class Tr>
-void launch_gradient(const void* logits, int64_t N, int64_t V, int64_t row_stride, const int32_t* ids, int32_t K, float scale, const float* rest_max,
-                     const float* rest_coef, const float* top_grad, float grad_out, const float* grad_scale, void* dlogits, hipStream_t st)
+void launch_dense(const void* logits, int64_t N, int64_t V, int64_t row_stride, float scale, const float* rest_max, const float* rest_coef,
+                  float grad_out, const float* grad_scale, void* dlogits, hipStream_t st)
 {
-    using elem = typename Tr::elem;
     const int64_t all = (V + Tr::kPerVec - 1) / Tr::kPerVec;
     hipLaunchKernelGGL((distill_dense_kernel<Tr>), rows_grid((unsigned)((all + kThreads - 1) / kThreads), N), dim3(kThreads), 0, st,
-                       (const elem*)logits, N, row_stride, (int32_t)V, scale, rest_max, rest_coef, grad_out, grad_scale, (elem*)dlogits);
-    hipLaunchKernelGGL((distill_top_kernel<Tr>), dim3((unsigned)((N * K + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, ids, top_grad, N,
-                       row_stride, (int32_t)V, K, grad_out, grad_scale, (elem*)dlogits);
+                       (const typename Tr::elem*)logits, N, row_stride, (int32_t)V, scale, rest_max, rest_coef, grad_out, grad_scale,
+                       (typename Tr::elem*)dlogits);
 }
 
-int32_t launch_forward(const void* logits, int32_t dt, const Layout& l, const DistillArgs& a, hipStream_t st)
+template <class Tr>
+void launch_top(int64_t N, int64_t V, int64_t row_stride, const int32_t* ids, int32_t K, const float* top_grad, float grad_out,
+                const float* grad_scale, void* dlogits, hipStream_t st)
 {
+    hipLaunchKernelGGL((distill_top_kernel<Tr>), dim3((unsigned)((N * K + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, ids, top_grad, N,
+                       row_stride, (int32_t)V, K, grad_out, grad_scale, (typename Tr::elem*)dlogits);
+}
+
+// The forward call, and with dlogits the gradient too.
+template <class Tr>
+int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const DistillArgs& a, hipStream_t st)
+{
+    using elem = typename Tr::elem;
     hipLaunchKernelGGL(distill_target_kernel, dim3((unsigned)((a.N + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
-    const bool ok = dt == ULORL_BF16 ? launch_pieces<StoreBF16>(l, logits, a, st) : launch_pieces<StoreF32>(l, logits, a, st);
-    if (!ok) return ULORL_ERR_HIP;
+    if (!launch_stream<Tr>(l, logits, dlogits, a, st)) return ULORL_ERR_HIP;
     const int64_t groups = (a.N + kWaves - 1) / kWaves;
-    hipLaunchKernelGGL(distill_finish_kernel, dim3((unsigned)(groups < kFinishGroups ? groups : kFinishGroups)), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((distill_finish_kernel<Tr>), dim3((unsigned)(groups < kFinishGroups ? groups : kFinishGroups)), dim3(kThreads), 0, st,
+                       (const elem*)logits, (elem*)dlogits, (int32_t)(kThreads * l.shape.vpt), a);
+    if (dlogits != nullptr) {
+        if (a.spin_limit == 0)
+            launch_dense<Tr>(logits, a.N, a.V, a.row_stride, a.scale, a.rest_max, a.rest_coef, a.grad_out, nullptr, dlogits, st);
+        launch_top<Tr>(a.N, a.V, a.row_stride, a.ids, a.K, a.top_grad, a.grad_out, nullptr, dlogits, st);
+    }
     return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
 }
 
@@ -595,7 +739,10 @@ int32_t distill_args(const void* logits, int32_t dt, int64_t N, int64_t V, int64
     a.target = (RowTarget*)(ws + l.target);
     a.slots = (unsigned long long*)(ws + l.slots);
     a.partial = (Partial*)(ws + l.partial);
-    a.ticket = (uint32_t*)(ws + l.ticket);
+    a.flags = (uint32_t*)(ws + l.flags);
+    a.pending = (unsigned long long*)(ws + l.pending);
+    a.spin_limit = 0;
+    a.grad_out = 1.0f;
     a.N = N; a.row_stride = row_stride; a.V = (int32_t)V; a.K = K; a.C = l.shape.pieces; a.tail = p->tail;
     a.inv_t = 1.0 / (double)p->temperature;
     a.scale = (float)(1.4426950408889634074 * a.inv_t);
@@ -623,7 +770,8 @@ int32_t ulorl_distill_fwd(const void* logits, int32_t dt, int64_t N, int64_t V, 
     const int32_t rc = distill_args(logits, dt, N, V, row_stride, teacher_ids, teacher_logp, K, weights, p, loss, kl, lse, rest_max, rest_coef,
                                     top_grad, counters, workspace, workspace_bytes, l, a);
     if (rc != ULORL_OK) return rc;
-    return launch_forward(logits, dt, l, a, (hipStream_t)hip_stream);
+    hipStream_t st = (hipStream_t)hip_stream;
+    return dt == ULORL_BF16 ? enqueue<StoreBF16>(logits, nullptr, l, a, st) : enqueue<StoreF32>(logits, nullptr, l, a, st);
 }
 
 int32_t ulorl_distill_bwd(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t row_stride, const int32_t* teacher_ids, int32_t K,
@@ -636,12 +784,13 @@ int32_t ulorl_distill_bwd(const void* logits, int32_t dt, int64_t N, int64_t V, 
     if (((uintptr_t)dlogits & 15u) != 0) return ULORL_ERR_ALIGN;
     if (!temperature_ok(temperature)) return ULORL_ERR_PARAM;
     const float scale = (float)(1.4426950408889634074 / (double)temperature);
-    if (dt == ULORL_BF16)
-        launch_gradient<StoreBF16>(logits, N, V, row_stride, teacher_ids, K, scale, rest_max, rest_coef, top_grad, grad_out, grad_scale, dlogits,
-                                   (hipStream_t)hip_stream);
-    else
-        launch_gradient<StoreF32>(logits, N, V, row_stride, teacher_ids, K, scale, rest_max, rest_coef, top_grad, grad_out, grad_scale, dlogits,
-                                  (hipStream_t)hip_stream);
+    hipStream_t st = (hipStream_t)hip_stream;
+    auto go = [&](auto tr) {
+        using Tr = decltype(tr);
+        launch_dense<Tr>(logits, N, V, row_stride, scale, rest_max, rest_coef, grad_out, grad_scale, dlogits, st);
+        launch_top<Tr>(N, V, row_stride, teacher_ids, K, top_grad, grad_out, grad_scale, dlogits, st);
+    };
+    if (dt == ULORL_BF16) go(StoreBF16{}); else go(StoreF32{});
     return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
 }
 
@@ -660,10 +809,10 @@ int32_t ulorl_distill_fwd_bwd(const void* logits, int32_t dt, int64_t N, int64_t
     LaunchOpts opts;
     rc = resolve_launch(launch, &opts);
     if (rc != ULORL_OK) return rc;
-    rc = launch_forward(logits, dt, l, a, (hipStream_t)hip_stream);
-    if (rc != ULORL_OK) return rc;
-    return ulorl_distill_bwd(logits, dt, N, V, row_stride, teacher_ids, K, p->temperature, rest_max, rest_coef, top_grad, grad_out, nullptr, dlogits,
-                             hip_stream);
+    if (l.cooperative && !opts.per_row) a.spin_limit = opts.sync_spins;
+    a.grad_out = grad_out;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return dt == ULORL_BF16 ? enqueue<StoreBF16>(logits, dlogits, l, a, st) : enqueue<StoreF32>(logits, dlogits, l, a, st);
 }
 
 }  // extern "C"

@@ -297,6 +297,30 @@ def test_in_place_and_strided(n, V, dtype):
         compare(dict(kl=r4.kl, lse=r4.lse, loss=r4.loss, dlogits=got), ref, tol, dtype)
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n,V", [(3, 40000), (40, 151936), (700, 32003)])
+def test_pieces_whose_wait_expires(n, V, dtype):
+    """A wait of one poll: what a workgroup leaves undone is written by the kernel that finishes the rows, in place too."""
+    z, ids, logp, w = problem(n, V, 40, dtype, 7, ragged=True)
+    w[0] = 0.0
+    p = ulorl.DistillParams()
+    short = ulorl.Launch(sync_spins=1)
+    check(z, ids, logp, w, p, ("one",), launch=short)
+    r, d = ulorl.distill_fwd_bwd(z, ids, logp, w, p)
+    r2, d2 = ulorl.distill_fwd_bwd(z, ids, logp, w, p, inplace=True, launch=short)
+    assert torch.equal(r.kl, r2.kl) and torch.equal(r.top_grad, r2.top_grad)
+    assert (d.float() - d2.float()).abs().max() <= 4 * HALF_STEP[dtype] * d.float().abs().max()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_two_passes_on_request(dtype):
+    z, ids, logp, w = problem(30, 70001, 40, dtype, 7)
+    check(z, ids, logp, w, ulorl.DistillParams(), ("one",), launch=ulorl.Launch(per_row=True))
+    r = ulorl.distill_fwd(z, ids, logp, w)
+    r2, d2 = ulorl.distill_fwd_bwd(z, ids, logp, w, launch=ulorl.Launch(per_row=True))
+    assert torch.equal(d2, ulorl.distill_bwd(z, ids, r)) and torch.equal(r.loss, r2.loss)
+
+
 def test_the_gradient_against_differences():
     """Along random directions u, |u| <= 1: (kl(z + h u) - kl(z - h u)) / 2h is off by h^2 / 6 times a third cumulant of u (at
     most 8, in each of two terms of mass at most 1) and by the rounding of the two divergences over 2h."""
