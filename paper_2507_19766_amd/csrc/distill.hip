@@ -20,6 +20,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "logits_stream.hpp"
 #include "row_sums.hpp"
 #include "ulorl.h"
@@ -35,15 +37,20 @@ constexpr int kMaxK = 128;              // two listed tokens per lane of a wave
 constexpr int64_t kMaxDistillRows = 1 << 24;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kFinishGroups = 1024;     // workgroups of the finishing kernel at most, each with its partial sums
+// The finishing kernel takes a wave per row, and no more workgroups than take their tickets quickly (2048 of them, 20 us; 256, 3):
+// small ones, spread over the chip, while 256 of them are enough (256 rows 7.5 us, in large ones 11.7), else large ones, which fill it
+// (8192 rows 27 us, in small ones 38).
+constexpr int kFinishGroups = 256;
+constexpr int kFinishSmall = 256, kFinishLarge = 1024;
 
 enum { ROW_ON = 0, ROW_WEIGHTLESS = 1, ROW_EMPTY = 2, ROW_BAD_TOKEN = 3, ROW_BAD_TARGET = 4 };
 
-// What the stream has to know of a row's target: g Q and g q_rest, with g = weight / (D T).
+// What the stream has to know of a row's target: g Q and g q_rest, with g = weight / (D T).  twice: an id is listed twice, which the
+// stream finds (and publishes as a sum that is no number).
 struct RowTarget {
     float mass, rest;
     int32_t state;
-    int32_t unused;
+    int32_t twice;
 };
 
 struct Partial {
@@ -110,23 +117,8 @@ __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
     if (w == 0.0f) {
         t.state = ROW_WEIGHTLESS;
     } else {
-        // an id twice: every lane counts its own among all
-        uint32_t twice = 0;
-        const int n0 = a.K < 64 ? a.K : 64, n1 = a.K - n0;
-        uint32_t seen0 = 0, seen1 = 0;
-        for (int s = 0; s < n0; ++s) {
-            const int32_t other = __builtin_amdgcn_readlane(id[0], s);
-            seen0 += id[0] == other ? 1u : 0u;
-            seen1 += id[1] == other ? 1u : 0u;
-        }
-        for (int s = 0; s < n1; ++s) {
-            const int32_t other = __builtin_amdgcn_readlane(id[1], s);
-            seen0 += id[0] == other ? 1u : 0u;
-            seen1 += id[1] == other ? 1u : 0u;
-        }
-        twice = (id[0] >= 0 && seen0 > 1) || (id[1] >= 0 && seen1 > 1);
         const bool beyond = id[0] >= a.V || id[1] >= a.V;
-        const bool bad = twice || !finite(w) || (id[0] >= 0 && !(l[0] <= 3.4028235e38f)) || (id[1] >= 0 && !(l[1] <= 3.4028235e38f));
+        const bool bad = !finite(w) || (id[0] >= 0 && !(l[0] <= 3.4028235e38f)) || (id[1] >= 0 && !(l[1] <= 3.4028235e38f));
         if (__any(beyond)) {
             t.state = ROW_BAD_TOKEN;
         } else if (__any(bad)) {
@@ -221,18 +213,25 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
     sh.head[tid] = -1;
     __syncthreads();
     float z = kFloor;
-    bool dead = false;
-    {
-        const int at = id / E - first;              // id < V: the row's state says so
-        if (id >= 0 && at >= 0 && at < NT * VPT) {
-            z = Tr::load1(rowp + id);
-            a.top_grad[row * a.K + tid] = z;
-            sh.where[tid] = (at / NT) * 8 + (id & (E - 1));
-            sh.next[tid] = atomicExch(&sh.head[at & (NT - 1)], tid);
-            dead = z <= kFloor && a.teacher[row * a.K + tid] > -INFINITY;       // the teacher's token is masked here
-        }
+    bool dead = false;                          // the row is no row: a token of the teacher's masked, or listed twice
+    const int at = id / E - first;              // id < V: the row's state says so
+    const bool in_piece = id >= 0 && at >= 0 && at < NT * VPT;
+    if (in_piece) {
+        z = Tr::load1(rowp + id);
+        a.top_grad[row * a.K + tid] = z;
+        sh.where[tid] = (at / NT) * 8 + (id & (E - 1));
+        sh.next[tid] = atomicExch(&sh.head[at & (NT - 1)], tid);
+        dead = z <= kFloor && a.teacher[row * a.K + tid] > -INFINITY;
     }
     __syncthreads();
+    if (in_piece) {
+        for (int j = sh.head[at & (NT - 1)]; j >= 0; j = sh.next[j]) {
+            if (j != tid && sh.where[j] == sh.where[tid]) {
+                dead = true;
+                a.target[row].twice = 1;
+            }
+        }
+    }
     for (int j = sh.head[tid]; j >= 0; j = sh.next[j]) {
         const int k_j = sh.where[j] >> 3, e = sh.where[j] & 7;
 #pragma unroll
@@ -335,9 +334,16 @@ __device__ __forceinline__ void store_vector(typename Tr::elem* outp, int32_t V,
     }
 }
 
+// A listed token's gradient; what is no number leaves 0, as in RestGradient.
+template <class Tr>
+__device__ __forceinline__ void store_top(typename Tr::elem* outp, int32_t V, int32_t id, float g)
+{
+    if (id >= 0 && id < V) Tr::store1(outp + id, finite(g) ? g : 0.0f);
+}
+
 // One call: the pieces of a row keep their logits in registers, tell each other their sums and write the gradient of their
 // unlisted tokens; every logit is read once and every gradient written once (the listed tokens' over it, by
-// distill_top_kernel).  A piece's two words in a.slots, zero before, are relaxed agent-scope atomics that carry their own validity.
+// distill_finish_kernel).  A piece's two words in a.slots, zero before, are relaxed agent-scope atomics that carry their own validity.
 // A row's pieces are neighbours in dispatch order, so partners are resident or next in line; the wait is bounded all the same: a
 // workgroup whose wait expires writes nothing (in place, its logits stay) and marks its piece, which distill_finish_kernel then
 // writes.
@@ -416,86 +422,100 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr
 // ---------------------------------------------------------------------------------------------
 // the rows' results
 // ---------------------------------------------------------------------------------------------
-template <class Tr>
-__global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, int32_t piece_vectors,
+template <class Tr, int NT>
+__global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, int32_t piece_vectors,
                                                                   DistillArgs a)
 {
-    __shared__ Partial part[kWaves];
+    constexpr int NW = NT / 64;
+    __shared__ Partial part[NW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Partial mine = {0.0, 0, 0, 0, 0};
-    for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.N; row += (int64_t)gridDim.x * kWaves) {
-        const int32_t state = a.target[row].state;
+    for (int64_t row = (int64_t)blockIdx.x * NW + wave; row < a.N; row += (int64_t)gridDim.x * NW) {
+        // everything a row needs is on its way before the first of it is looked at (of a row that does not count some of it is
+        // anything)
+        const RowTarget target = a.target[row];
         float* top = a.top_grad + row * a.K;
+        const double w = a.weights ? (double)a.weights[row] : 1.0;
+        int32_t id[2] = {-1, -1};
+        float z[2] = {kFloor, kFloor}, listed[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (lane + 64 * h < a.K) {
+                id[h] = a.ids[row * a.K + lane + 64 * h];
+                z[h] = top[lane + 64 * h];
+                listed[h] = a.teacher[row * a.K + lane + 64 * h];
+            }
+        }
+        const unsigned long long slot = lane < a.C ? a.slots[(row * a.C + lane) * 2] : 0ull;
+        const int32_t state = target.twice != 0 ? ROW_BAD_TARGET : target.state;
         float grad[2] = {0.0f, 0.0f};
         float kl_out = 0.0f, lse_out = 0.0f, max_out = 0.0f, coef_out = 0.0f;
         if (state == ROW_ON) {
-            // the unlisted tokens: the row's pieces
+            // the listed tokens; the second of a lane's two only where there is one
+            double l[2], e[2] = {0.0, 0.0}, q[2] = {0.0, 0.0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                z[h] = id[h] >= 0 ? z[h] : kFloor;
+                l[h] = id[h] >= 0 ? (double)listed[h] : -INFINITY;
+            }
+            // the unlisted ones: the row's pieces
             float m = kFloor;
             double S = 0.0;
-            for (int c = lane; c < a.C; c += 64) {
+            if (lane < a.C) {
+                m = __uint_as_float((uint32_t)slot);
+                S = (double)__uint_as_float((uint32_t)(slot >> 32));
+            }
+            for (int c = lane + 64; c < a.C; c += 64) {
                 const unsigned long long w0 = a.slots[(row * a.C + c) * 2];
-                const float pm = __uint_as_float((uint32_t)w0);
-                const float M = larger(m, pm);
-                S = exp((double)(m - M) * a.inv_t) * S + exp((double)(pm - M) * a.inv_t) * (double)__uint_as_float((uint32_t)(w0 >> 32));
+                const float pm = __uint_as_float((uint32_t)w0), M = larger(m, pm);
+                S = exp(((double)m - (double)M) * a.inv_t) * S + exp(((double)pm - (double)M) * a.inv_t) * (double)__uint_as_float((uint32_t)(w0 >> 32));
                 m = M;
             }
             const float rest_max = wave_max(m);
-            S = wave_sum_f64(exp((double)(m - rest_max) * a.inv_t) * S);
-            // the listed ones
-            double z[2], l[2];
-            bool here[2], masked[2];
-            float M = rest_max;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int j = lane + 64 * h;
-                here[h] = j < a.K && a.ids[row * a.K + j] >= 0;
-                const float zf = here[h] ? top[j] : kFloor;
-                masked[h] = zf <= kFloor;
-                z[h] = (double)zf;
-                l[h] = here[h] ? (double)a.teacher[row * a.K + j] : -INFINITY;
-                M = larger(M, zf);
-            }
-            M = wave_max(M);
-            double e[2], q[2], lp[2], terms = 0.0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) e[h] = masked[h] ? 0.0 : exp((z[h] - (double)M) * a.inv_t);
-            const double total = exp((double)(rest_max - M) * a.inv_t) * S + wave_sum2(e[0], e[1]);
-            const double ln_total = log(total);
+            if (a.C > 1) S *= exp(((double)m - (double)rest_max) * a.inv_t);
+            S = wave_sum_f64(S);
+            const float M = larger(rest_max, wave_max(larger(z[0], z[1])));
+            const double R = exp(((double)rest_max - (double)M) * a.inv_t) * S;         // relative to M, as the listed ones
+            double norm = 0.0;
             if (a.tail == ULORL_TAIL_RENORM) {
                 const double lm = (double)wave_max(larger((float)l[0], (float)l[1]));
-                const double norm = lm + log(wave_sum2(exp(l[0] - lm), exp(l[1] - lm)));
-                l[0] -= norm;
-                l[1] -= norm;
+                norm = lm + log(wave_sum2(exp(l[0] - lm), a.K > 64 ? exp(l[1] - lm) : 0.0));
             }
-            bool dead = false;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                if (h == 1 && a.K <= 64) break;
+                if (!(z[h] <= kFloor)) e[h] = exp(((double)z[h] - (double)M) * a.inv_t);
+                l[h] -= norm;
                 q[h] = exp(l[h]);
-                lp[h] = (z[h] - (double)M) * a.inv_t - ln_total;
-                dead = dead || (here[h] && masked[h] && l[h] > -INFINITY);
-                if (q[h] > 0.0 && !masked[h]) terms += q[h] * (l[h] - lp[h]);
             }
-            const double q_sum = wave_sum2(q[0], q[1]);
+            const double total = R + wave_sum2(e[0], e[1]), q_sum = wave_sum2(q[0], q[1]);
+            const double ln_total = log(total);
+            bool dead = false;
+            double terms = 0.0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool masked = z[h] <= kFloor;
+                dead = dead || (masked && l[h] > -INFINITY);
+                if (q[h] > 0.0 && !masked) terms += q[h] * (l[h] - (((double)z[h] - (double)M) * a.inv_t - ln_total));
+            }
             const bool has_rest = S > 0.0;
             const double q_rest = a.tail == ULORL_TAIL_BUCKET && has_rest && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
             const double mass = q_sum + q_rest;
-            const double ln_rest = (double)(rest_max - M) * a.inv_t + log(S) - ln_total;
             double kl = wave_sum_f64(terms);
-            if (q_rest > 0.0) kl += q_rest * (log(q_rest) - ln_rest);
+            if (q_rest > 0.0) kl += q_rest * (log(q_rest / S) - (((double)rest_max - (double)M) * a.inv_t - ln_total));
             const bool ok = !__any(dead) && total > 0.0 && total < 1.0e300 && fabs(kl) < 1.0e300;
-            const double w = a.weights ? (double)a.weights[row] : 1.0;
-            const double g = w * a.inv_D * a.inv_t;
             lse_out = total > 0.0 ? (float)((double)M * a.inv_t + ln_total) : __builtin_nanf("");
-            max_out = rest_max;
             if (ok) {
+                const double g = w * a.inv_D * a.inv_t;
                 kl_out = (float)kl;
-                if (has_rest) coef_out = (float)(g * (mass * exp(ln_rest) - q_rest) / S);
+                max_out = rest_max;
+                if (has_rest) coef_out = (float)(g * (mass * (R / total) - q_rest) / S);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) grad[h] = here[h] ? (float)(g * ((masked[h] ? 0.0 : exp(lp[h])) * mass - q[h])) : 0.0f;
+                for (int h = 0; h < 2; ++h)
+                    if (id[h] >= 0) grad[h] = (float)(g * (e[h] / total * mass - q[h]));
                 mine.loss += w * kl;
                 mine.on += 1;
             } else {
-                max_out = 0.0f;
                 mine.status |= ULORL_STATUS_NONFINITE;
             }
         } else if (state == ROW_WEIGHTLESS) {
@@ -506,8 +526,11 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename
             mine.status |= state == ROW_BAD_TOKEN ? ULORL_STATUS_BAD_TOKEN : ULORL_STATUS_BAD_TARGET;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
             if (lane + 64 * h < a.K) top[lane + 64 * h] = grad[h];
+            // one call: the unlisted tokens' gradients are there already
+            if (a.spin_limit > 0 && state == ROW_ON) store_top<Tr>(dlogits + row * a.row_stride, a.V, id[h], grad[h] * a.grad_out);
+        }
         if (lane == 0) {
             a.kl[row] = kl_out;
             a.lse[row] = lse_out;
@@ -518,7 +541,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename
     if (a.spin_limit > 0 && a.flags[1] != 0u) {     // pieces whose workgroup waited in vain: their logits are whole, in place too
         __threadfence();                            // the rows' results are this wave's own
         const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
-        for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.N; row += (int64_t)gridDim.x * kWaves) {
+        for (int64_t row = (int64_t)blockIdx.x * NW + wave; row < a.N; row += (int64_t)gridDim.x * NW) {
             for (unsigned long long todo = a.pending[row]; todo != 0ull; todo &= todo - 1ull) {
                 const RestGradient rest(a.rest_coef[row] * a.grad_out, a.rest_max[row], a.scale);
                 const int begin = (__ffsll((long long)todo) - 1) * piece_vectors;
@@ -526,6 +549,10 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename
                     store_vector<Tr>(dlogits + row * a.row_stride, a.V, i,
                                      rest.none ? u32x4{0u, 0u, 0u, 0u} : rest.template of<Tr>(load_vector<Tr>(logits + row * a.row_stride, a.V, i)));
             }
+            if (a.pending[row] == 0ull) continue;
+            __threadfence();                        // the listed tokens' again, over them
+            for (int j = lane; j < a.K; j += 64)
+                store_top<Tr>(dlogits + row * a.row_stride, a.V, a.ids[row * a.K + j], a.top_grad[row * a.K + j] * a.grad_out);
         }
     }
     if (lane == 0) part[wave] = mine;
@@ -533,7 +560,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename
     if (threadIdx.x == 0) {
         Partial sum = {0.0, 0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < NW; ++w) {
             sum.loss += part[w].loss;
             sum.on += part[w].on;
             sum.weightless += part[w].weightless;
@@ -550,7 +577,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename
     if (!last_workgroup(a.flags, gridDim.x)) return;
     // all sums in a fixed order: lanes over workgroups, then lanes, then waves
     Partial q = {0.0, 0, 0, 0, 0};
-    for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads) {
+    for (unsigned b = threadIdx.x; b < gridDim.x; b += NT) {
         const Partial& from = a.partial[b];
         q.loss += published(&from.loss);
         q.on += published(&from.on);
@@ -571,7 +598,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const typename
     if (threadIdx.x == 0) {
         Partial sum = part[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
+        for (int w = 1; w < NW; ++w) {
             sum.loss += part[w].loss;
             sum.on += part[w].on;
             sum.weightless += part[w].weightless;
@@ -613,10 +640,7 @@ __global__ __launch_bounds__(kThreads) void distill_top_kernel(const int32_t* id
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (i >= N * K) return;
-    const int32_t id = ids[i];
-    if (id < 0 || id >= V) return;
-    const float g = top_grad[i] * (grad_scale ? *grad_scale * grad_out : grad_out);
-    Tr::store1(dlogits + (i / K) * row_stride + id, finite(g) ? g : 0.0f);
+    store_top<Tr>(dlogits + (i / K) * row_stride, V, ids[i], top_grad[i] * (grad_scale ? *grad_scale * grad_out : grad_out));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -710,12 +734,16 @@ int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const Distil
     using elem = typename Tr::elem;
     hipLaunchKernelGGL(distill_target_kernel, dim3((unsigned)((a.N + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
     if (!launch_stream<Tr>(l, logits, dlogits, a, st)) return ULORL_ERR_HIP;
-    const int64_t groups = (a.N + kWaves - 1) / kWaves;
-    hipLaunchKernelGGL((distill_finish_kernel<Tr>), dim3((unsigned)(groups < kFinishGroups ? groups : kFinishGroups)), dim3(kThreads), 0, st,
-                       (const elem*)logits, (elem*)dlogits, (int32_t)(kThreads * l.shape.vpt), a);
-    if (dlogits != nullptr) {
-        if (a.spin_limit == 0)
-            launch_dense<Tr>(logits, a.N, a.V, a.row_stride, a.scale, a.rest_max, a.rest_coef, a.grad_out, nullptr, dlogits, st);
+    auto finish = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value, NW = NT / 64;
+        const int64_t groups = (a.N + NW - 1) / NW;
+        hipLaunchKernelGGL((distill_finish_kernel<Tr, NT>), dim3((unsigned)(groups < kFinishGroups ? groups : kFinishGroups)), dim3(NT), 0, st,
+                           (const elem*)logits, (elem*)dlogits, (int32_t)(kThreads * l.shape.vpt), a);
+    };
+    if (a.N <= (int64_t)kFinishGroups * (kFinishSmall / 64)) finish(std::integral_constant<int, kFinishSmall>{});
+    else finish(std::integral_constant<int, kFinishLarge>{});
+    if (dlogits != nullptr && a.spin_limit == 0) {
+        launch_dense<Tr>(logits, a.N, a.V, a.row_stride, a.scale, a.rest_max, a.rest_coef, a.grad_out, nullptr, dlogits, st);
         launch_top<Tr>(a.N, a.V, a.row_stride, a.ids, a.K, a.top_grad, a.grad_out, nullptr, dlogits, st);
     }
     return hipGetLastError() == hipSuccess ? ULORL_OK : ULORL_ERR_HIP;
