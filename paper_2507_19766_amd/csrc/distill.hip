@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
             const double g = (double)w * a.inv_D * a.inv_t;
             double mass = 1.0, rest = 0.0;
             if (a.tail != ULORL_TAIL_RENORM) {
-                const double q = wave_sum2(exp((double)l[0]), exp((double)l[1]));
+                const double q = wave_sum2(exp64((double)l[0]), a.K > 64 ? exp64((double)l[1]) : 0.0);
                 rest = a.tail == ULORL_TAIL_BUCKET && q < 1.0 ? 1.0 - q : 0.0;
                 mass = q + rest;
             }
@@ -191,8 +191,9 @@ struct PieceSums {
     double S, top_S;            // relative to them
 };
 
-// A row's piece c into registers (v) without its listed tokens, whose logits go to a.top_grad, and its sums (thread 0).
-template <class Tr, int VPT>
+// A row's piece c into registers (v) without its listed tokens, whose logits go to a.top_grad, and its sums (thread 0).  TOP: the listed
+// tokens' sum is wanted too.
+template <class Tr, int VPT, bool TOP>
 __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT], PieceShared& sh)
 {
     constexpr int NT = kThreads, E = Tr::kPerVec;
@@ -241,31 +242,37 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
 
     Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
     absorb_rest<Tr, VPT, 0>(v, a.scale, acc);
-    const float wm = wave_max(acc.m), wt = wave_max(z);
+    const float wm = wave_max(acc.m);
     // z scale - mL differs from (z - m) scale by the rounding of mL: taken out here (nothing to take out of an empty lane)
     const float d = fmaf(acc.m - wm, a.scale, -fmaf(acc.m, a.scale, -acc.mL));
     const double S = acc.S == 0.0f ? 0.0 : (double)fast_exp2(d) * ((double)acc.S + (double)acc.Sc);
-    double top = z > kFloor ? (double)fast_exp2((z - wt) * a.scale) : 0.0;
-    if (z != z || dead) top = (double)__builtin_nanf("");
-    const double wS = wave_sum_f64(S), wT = wave_sum_f64(top);
+    const double wS = wave_sum_f64(S);
     if ((tid & 63) == 0) {
         sh.m[wave] = wm;
         sh.S[wave] = wS;
-        sh.top_m[wave] = wt;
-        sh.top_S[wave] = wT;
+    }
+    if constexpr (TOP) {
+        const float wt = wave_max(z);
+        double top = z > kFloor ? (double)fast_exp2((z - wt) * a.scale) : 0.0;
+        if (z != z || dead) top = (double)__builtin_nanf("");
+        top = wave_sum_f64(top);
+        if ((tid & 63) == 0) {
+            sh.top_m[wave] = wt;
+            sh.top_S[wave] = top;
+        }
     }
     __syncthreads();
-    PieceSums p = {sh.m[0], sh.top_m[0], 0.0, 0.0};
+    PieceSums p = {kFloor, kFloor, 0.0, 0.0};
     if (tid == 0) {
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-            p.m = larger(p.m, sh.m[w]);
-            p.top_m = larger(p.top_m, sh.top_m[w]);
-        }
+        for (int w = 0; w < kWaves; ++w) p.m = larger(p.m, sh.m[w]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            p.S += (double)fast_exp2((sh.m[w] - p.m) * a.scale) * sh.S[w];
-            p.top_S += (double)fast_exp2((sh.top_m[w] - p.top_m) * a.scale) * sh.top_S[w];
+        for (int w = 0; w < kWaves; ++w) p.S += (double)fast_exp2((sh.m[w] - p.m) * a.scale) * sh.S[w];
+        if constexpr (TOP) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) p.top_m = larger(p.top_m, sh.top_m[w]);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) p.top_S += (double)fast_exp2((sh.top_m[w] - p.top_m) * a.scale) * sh.top_S[w];
         }
     }
     return p;
@@ -284,11 +291,10 @@ __global__ __launch_bounds__(kThreads) void distill_piece_kernel(const typename 
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
     if (row >= a.N || a.target[row].state != ROW_ON) return;
     u32x4 v[VPT];
-    const PieceSums p = piece_sums<Tr, VPT>(a, logits + row * a.row_stride, row, (int)blockIdx.x, v, sh);
+    const PieceSums p = piece_sums<Tr, VPT, false>(a, logits + row * a.row_stride, row, (int)blockIdx.x, v, sh);
     if (threadIdx.x == 0) {
         unsigned long long* slot = a.slots + (row * a.C + blockIdx.x) * 2;
         slot[0] = slot_word(p.m, p.S);
-        slot[1] = slot_word(p.top_m, p.top_S);
     }
 }
 
@@ -375,7 +381,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr
         store_all([&](int) { return zero; });
         return;
     }
-    const PieceSums p = piece_sums<Tr, VPT>(a, logits + row * a.row_stride, row, c, v, sh);
+    const PieceSums p = piece_sums<Tr, VPT, true>(a, logits + row * a.row_stride, row, c, v, sh);
     if (tid < 64) {
         unsigned long long* slot = a.slots + row * a.C * 2;
         unsigned long long w0 = slot_word(p.m, p.S), w1 = slot_word(p.top_m, p.top_S);
@@ -468,28 +474,28 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
             for (int c = lane + 64; c < a.C; c += 64) {
                 const unsigned long long w0 = a.slots[(row * a.C + c) * 2];
                 const float pm = __uint_as_float((uint32_t)w0), M = larger(m, pm);
-                S = exp(((double)m - (double)M) * a.inv_t) * S + exp(((double)pm - (double)M) * a.inv_t) * (double)__uint_as_float((uint32_t)(w0 >> 32));
+                S = exp64(((double)m - (double)M) * a.inv_t) * S + exp64(((double)pm - (double)M) * a.inv_t) * (double)__uint_as_float((uint32_t)(w0 >> 32));
                 m = M;
             }
             const float rest_max = wave_max(m);
-            if (a.C > 1) S *= exp(((double)m - (double)rest_max) * a.inv_t);
+            if (a.C > 1) S *= exp64(((double)m - (double)rest_max) * a.inv_t);
             S = wave_sum_f64(S);
             const float M = larger(rest_max, wave_max(larger(z[0], z[1])));
-            const double R = exp(((double)rest_max - (double)M) * a.inv_t) * S;         // relative to M, as the listed ones
+            const double R = exp64(((double)rest_max - (double)M) * a.inv_t) * S;         // relative to M, as the listed ones
             double norm = 0.0;
             if (a.tail == ULORL_TAIL_RENORM) {
                 const double lm = (double)wave_max(larger((float)l[0], (float)l[1]));
-                norm = lm + log(wave_sum2(exp(l[0] - lm), a.K > 64 ? exp(l[1] - lm) : 0.0));
+                norm = lm + log64(wave_sum2(exp64(l[0] - lm), a.K > 64 ? exp64(l[1] - lm) : 0.0));
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (h == 1 && a.K <= 64) break;
-                if (!(z[h] <= kFloor)) e[h] = exp(((double)z[h] - (double)M) * a.inv_t);
+                if (!(z[h] <= kFloor)) e[h] = exp64(((double)z[h] - (double)M) * a.inv_t);
                 l[h] -= norm;
-                q[h] = exp(l[h]);
+                q[h] = exp64(l[h]);
             }
             const double total = R + wave_sum2(e[0], e[1]), q_sum = wave_sum2(q[0], q[1]);
-            const double ln_total = log(total);
+            const double ln_total = log64(total), per_total = 1.0 / total, per_S = 1.0 / S;
             bool dead = false;
             double terms = 0.0;
 #pragma unroll
@@ -502,17 +508,17 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
             const double q_rest = a.tail == ULORL_TAIL_BUCKET && has_rest && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
             const double mass = q_sum + q_rest;
             double kl = wave_sum_f64(terms);
-            if (q_rest > 0.0) kl += q_rest * (log(q_rest / S) - (((double)rest_max - (double)M) * a.inv_t - ln_total));
+            if (q_rest > 0.0) kl += q_rest * (log64(q_rest * per_S) - (((double)rest_max - (double)M) * a.inv_t - ln_total));
             const bool ok = !__any(dead) && total > 0.0 && total < 1.0e300 && fabs(kl) < 1.0e300;
             lse_out = total > 0.0 ? (float)((double)M * a.inv_t + ln_total) : __builtin_nanf("");
             if (ok) {
                 const double g = w * a.inv_D * a.inv_t;
                 kl_out = (float)kl;
                 max_out = rest_max;
-                if (has_rest) coef_out = (float)(g * (mass * (R / total) - q_rest) / S);
+                if (has_rest) coef_out = (float)(g * (mass * (R * per_total) - q_rest) * per_S);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    if (id[h] >= 0) grad[h] = (float)(g * (e[h] / total * mass - q[h]));
+                    if (id[h] >= 0) grad[h] = (float)(g * (e[h] * per_total * mass - q[h]));
                 mine.loss += w * kl;
                 mine.on += 1;
             } else {

@@ -107,6 +107,37 @@ __device__ __forceinline__ u32x4 load_vector(const typename Tr::elem* rowp, int3
     return v;
 }
 
+// e^x and ln x in 64 bits, to a few units of the last place, in a third of the instructions of the library's functions: they are
+// most of what finishing a row costs.  x = (n + f) ln 2 with |f| <= 1/2, and the Taylor series of 2^f up to f^12 (the next term is below
+// 2e-16).  exp64: not-a-number stays, below e^-1100 is 0.
+__device__ __forceinline__ double exp64(double x)
+{
+    x = x < -1100.0 ? -1100.0 : x;
+    // x log2(e) in two parts: the rounding of one product would be |x| units of the last place
+    const double hi = x * 1.4426950408889634, n = rint(hi);
+    const double f = fma(x, 1.4426950408889634, -n) + x * 2.0355273740931033e-17;
+    double p = 2.5678435993488196e-11;
+    p = fma(p, f, 4.44553827187081e-10);
+    p = fma(p, f, 7.054911620801121e-09);
+    p = fma(p, f, 1.0178086009239696e-07);
+    p = fma(p, f, 1.3215486790144305e-06);
+    p = fma(p, f, 1.5252733804059838e-05);
+    p = fma(p, f, 0.00015403530393381606);
+    p = fma(p, f, 0.0013333558146428441);
+    p = fma(p, f, 0.009618129107628477);
+    p = fma(p, f, 0.055504108664821576);
+    p = fma(p, f, 0.2402265069591007);
+    p = fma(p, f, 0.6931471805599453);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+// One Newton step from the 32-bit logarithm: its error squared.  For x within the range of 32 bits.
+__device__ __forceinline__ double log64(double x)
+{
+    const double l = (double)__builtin_amdgcn_logf((float)x) * 0.69314718055994530942;
+    return l + fma(x, exp64(-l), -1.0);
+}
+
 }  // namespace ulorl_detail
 
 #endif

@@ -486,7 +486,7 @@ __device__ __forceinline__ void finish_row(const TopkArgs& a, const typename Tr:
     const int all = (a.V + E - 1) / E, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
     const bool ok = st.m > kFloor && st.S >= 0.5 && st.S < 1.0e30;       // neither NaN, +infinity nor everything masked
     if (threadIdx.x == 0) {
-        const double ln_s = log(st.S);
+        const double ln_s = log64(st.S);
         sh.ln_s = ln_s;
         const float nan = __builtin_nanf("");
         a.lse[row] = ok ? (float)((double)st.m * a.inv_t + ln_s) : nan;
