@@ -284,8 +284,13 @@ __device__ __forceinline__ unsigned long long slot_word(float m, double S)
     return ((unsigned long long)__float_as_uint((float)S) << 32) | __float_as_uint(m);
 }
 
+// Large bf16 pieces: four workgroups a compute unit at most, which keeps the chip's window of addresses narrow (8192 x 151936: 398 us with
+// the six that would fit, 399 with five, 386 with four); small ones and fp32 take what fits (3001 x 32000: 53 us, with four 62).
 template <class Tr, int VPT>
-__global__ __launch_bounds__(kThreads) void distill_piece_kernel(const typename Tr::elem* logits, DistillArgs a)
+constexpr int kMostWaves = Tr::kPerVec == 8 && VPT >= 11 ? 4 : 8;
+
+template <class Tr, int VPT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, kMostWaves<Tr, VPT>))) void distill_piece_kernel(const typename Tr::elem* logits, DistillArgs a)
 {
     __shared__ PieceShared sh;
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
