@@ -10,10 +10,10 @@
 // the listed probabilities would lose all its digits where the student is sure of them.  What a row is made of after that (K terms)
 // is in 64 bits: a divergence is a small sum of larger terms.
 //
-//   distill_target_kernel   one wave per row: is the target a distribution; what the row's gradient needs of it
+//   distill_target_kernel   is the target a distribution; what the row's gradient needs of it
 //   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers, to (max, S); listed logits
 //   distill_row_kernel      one call: the same pieces, which tell each other their sums and write the gradient from the registers
-//   distill_finish_kernel   one wave per row: kl, the listed tokens' gradients, the unlisted ones' coefficient; the loss
+//   distill_finish_kernel   kl, the listed tokens' gradients, the unlisted ones' coefficient; the loss
 //   distill_dense_kernel    the gradient of all tokens as if unlisted, one 16-byte vector per thread
 //   distill_top_kernel      the listed tokens' gradients over it
 #include <hip/hip_runtime.h>
@@ -37,7 +37,7 @@ constexpr int kMaxK = 128;              // two listed tokens per lane of a wave
 constexpr int64_t kMaxDistillRows = 1 << 24;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-// The finishing kernel takes a wave per row, and no more workgroups than take their tickets quickly (2048 of them, 20 us; 256, 3):
+// The finishing kernel takes no more workgroups than take their tickets quickly (2048 of them, 20 us; 256, 3):
 // small ones, spread over the chip, while 256 of them are enough (256 rows 7.5 us, in large ones 11.7), else large ones, which fill it
 // (8192 rows 27 us, in small ones 38).
 constexpr int kFinishGroups = 256;
@@ -83,33 +83,66 @@ struct DistillArgs {
     double inv_t, inv_D;
 };
 
-// Two values per lane of a wave, listed tokens lane and lane + 64.
-__device__ __forceinline__ double wave_sum2(double a, double b) { return wave_sum_f64(a + b); }
+// A row's K terms are worked on by L lanes, two terms each: 16, 32 or 64 as K asks, so that a wave takes up to four rows (what is
+// the same for all of a row's terms costs a wave the same however many rows it has).  Sums and maxima over the row's lanes, in
+// each of them, in a fixed order.
+template <int L>
+struct Lanes {
+    static_assert(L == 16 || L == 32 || L == 64, "whole rows of 16 lanes");
+    template <int CTRL>
+    static __device__ __forceinline__ double add(double x)
+    {
+        const int lo = __builtin_amdgcn_mov_dpp(__double2loint(x), CTRL, 0xF, 0xF, true), hi = __builtin_amdgcn_mov_dpp(__double2hiint(x), CTRL, 0xF, 0xF, true);
+        return x + __hiloint2double(hi, lo);
+    }
+    static __device__ __forceinline__ double sum(double x)
+    {
+        if constexpr (L == 64) return wave_sum_f64(x);
+        x = add<kMirror16>(add<kMirror8>(add<kXor2>(add<kXor1>(x))));
+        if constexpr (L == 32) x += __shfl_xor(x, 16);
+        return x;
+    }
+    static __device__ __forceinline__ float max(float x)
+    {
+        if constexpr (L == 64) return wave_max(x);
+        x = larger(x, from_lane<kXor1>(x));
+        x = larger(x, from_lane<kXor2>(x));
+        x = larger(x, from_lane<kMirror8>(x));
+        x = larger(x, from_lane<kMirror16>(x));
+        if constexpr (L == 32) x = larger(x, __shfl_xor(x, 16));
+        return x;
+    }
+    static __device__ __forceinline__ bool any(bool b)
+    {
+        const uint64_t row = L == 64 ? ~0ull : ((1ull << (L & 63)) - 1ull) << (threadIdx.x & 63 & ~(L - 1));
+        return (__ballot(b) & row) != 0ull;
+    }
+};
+inline int lanes_of(int K) { return K <= 32 ? 16 : K <= 64 ? 32 : 64; }
 
 // ---------------------------------------------------------------------------------------------
 // the targets
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
 
+template <int L>
 __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & (L - 1);
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / L) + (int)threadIdx.x / L;
     if (blockIdx.x == 0 && threadIdx.x < 2) a.flags[threadIdx.x] = 0u;
     if (row >= a.N) return;
     if (a.spin_limit > 0) {         // the exchange of the one-call path starts from zeros
         if (lane == 0) a.pending[row] = 0ull;
-        if (a.C > 1 && lane < a.C) {
-            a.slots[(row * a.C + lane) * 2] = 0ull;
-            a.slots[(row * a.C + lane) * 2 + 1] = 0ull;
-        }
+        if (a.C > 1)
+            for (int k = lane; k < 2 * a.C; k += L) a.slots[row * a.C * 2 + k] = 0ull;
     }
     const float w = a.weights ? a.weights[row] : 1.0f;
     int32_t id[2];
     float l[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int j = lane + 64 * h;
+        const int j = lane + L * h;
         id[h] = j < a.K ? a.ids[row * a.K + j] : -1;
         l[h] = id[h] >= 0 ? a.teacher[row * a.K + j] : -INFINITY;
     }
@@ -119,17 +152,17 @@ __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
     } else {
         const bool beyond = id[0] >= a.V || id[1] >= a.V;
         const bool bad = !finite(w) || (id[0] >= 0 && !(l[0] <= 3.4028235e38f)) || (id[1] >= 0 && !(l[1] <= 3.4028235e38f));
-        if (__any(beyond)) {
+        if (Lanes<L>::any(beyond)) {
             t.state = ROW_BAD_TOKEN;
-        } else if (__any(bad)) {
+        } else if (Lanes<L>::any(bad)) {
             t.state = ROW_BAD_TARGET;
-        } else if (!__any(id[0] >= 0 || id[1] >= 0) || (a.tail == ULORL_TAIL_RENORM && !__any(l[0] > -INFINITY || l[1] > -INFINITY))) {
+        } else if (!Lanes<L>::any(id[0] >= 0 || id[1] >= 0) || (a.tail == ULORL_TAIL_RENORM && !Lanes<L>::any(l[0] > -INFINITY || l[1] > -INFINITY))) {
             t.state = ROW_EMPTY;
         } else {
             const double g = (double)w * a.inv_D * a.inv_t;
             double mass = 1.0, rest = 0.0;
             if (a.tail != ULORL_TAIL_RENORM) {
-                const double q = wave_sum2(exp64((double)l[0]), a.K > 64 ? exp64((double)l[1]) : 0.0);
+                const double q = Lanes<L>::sum(exp64((double)l[0]) + (a.K > L ? exp64((double)l[1]) : 0.0));
                 rest = a.tail == ULORL_TAIL_BUCKET && q < 1.0 ? 1.0 - q : 0.0;
                 mass = q + rest;
             }
@@ -433,15 +466,42 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr
 // ---------------------------------------------------------------------------------------------
 // the rows' results
 // ---------------------------------------------------------------------------------------------
-template <class Tr, int NT>
+// Over a wave, in each lane: lanes in a fixed order, counts below 2^53 exactly.
+__device__ __forceinline__ void wave_partial(Partial& p)
+{
+    p.loss = wave_sum_f64(p.loss);
+    p.on = (int64_t)wave_sum_f64((double)p.on);
+    p.weightless = (int64_t)wave_sum_f64((double)p.weightless);
+    p.empty = (int64_t)wave_sum_f64((double)p.empty);
+    int64_t status = 0;
+#pragma unroll
+    for (int bit = 1; bit <= ULORL_STATUS_BAD_TARGET; bit <<= 1) status |= __any((p.status & bit) != 0) ? bit : 0;
+    p.status = status;
+}
+template <int NW>
+__device__ __forceinline__ Partial all_partials(const Partial* part)
+{
+    Partial sum = part[0];
+    for (int w = 1; w < NW; ++w) {
+        sum.loss += part[w].loss;
+        sum.on += part[w].on;
+        sum.weightless += part[w].weightless;
+        sum.empty += part[w].empty;
+        sum.status |= part[w].status;
+    }
+    return sum;
+}
+
+template <class Tr, int NT, int L>
 __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, int32_t piece_vectors,
                                                                   DistillArgs a)
 {
     constexpr int NW = NT / 64;
     __shared__ Partial part[NW];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int ROWS = NT / L;                 // at a time
+    const int lane = threadIdx.x & (L - 1);
     Partial mine = {0.0, 0, 0, 0, 0};
-    for (int64_t row = (int64_t)blockIdx.x * NW + wave; row < a.N; row += (int64_t)gridDim.x * NW) {
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + (int)threadIdx.x / L; row < a.N; row += (int64_t)gridDim.x * ROWS) {
         // everything a row needs is on its way before the first of it is looked at (of a row that does not count some of it is
         // anything)
         const RowTarget target = a.target[row];
@@ -451,10 +511,10 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
         float z[2] = {kFloor, kFloor}, listed[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (lane + 64 * h < a.K) {
-                id[h] = a.ids[row * a.K + lane + 64 * h];
-                z[h] = top[lane + 64 * h];
-                listed[h] = a.teacher[row * a.K + lane + 64 * h];
+            if (lane + L * h < a.K) {
+                id[h] = a.ids[row * a.K + lane + L * h];
+                z[h] = top[lane + L * h];
+                listed[h] = a.teacher[row * a.K + lane + L * h];
             }
         }
         const unsigned long long slot = lane < a.C ? a.slots[(row * a.C + lane) * 2] : 0ull;
@@ -476,30 +536,30 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
                 m = __uint_as_float((uint32_t)slot);
                 S = (double)__uint_as_float((uint32_t)(slot >> 32));
             }
-            for (int c = lane + 64; c < a.C; c += 64) {
+            for (int c = lane + L; c < a.C; c += L) {
                 const unsigned long long w0 = a.slots[(row * a.C + c) * 2];
                 const float pm = __uint_as_float((uint32_t)w0), M = larger(m, pm);
                 S = exp64(((double)m - (double)M) * a.inv_t) * S + exp64(((double)pm - (double)M) * a.inv_t) * (double)__uint_as_float((uint32_t)(w0 >> 32));
                 m = M;
             }
-            const float rest_max = wave_max(m);
+            const float rest_max = Lanes<L>::max(m);
             if (a.C > 1) S *= exp64(((double)m - (double)rest_max) * a.inv_t);
-            S = wave_sum_f64(S);
-            const float M = larger(rest_max, wave_max(larger(z[0], z[1])));
+            S = Lanes<L>::sum(S);
+            const float M = larger(rest_max, Lanes<L>::max(larger(z[0], z[1])));
             const double R = exp64(((double)rest_max - (double)M) * a.inv_t) * S;         // relative to M, as the listed ones
             double norm = 0.0;
             if (a.tail == ULORL_TAIL_RENORM) {
-                const double lm = (double)wave_max(larger((float)l[0], (float)l[1]));
-                norm = lm + log64(wave_sum2(exp64(l[0] - lm), a.K > 64 ? exp64(l[1] - lm) : 0.0));
+                const double lm = (double)Lanes<L>::max(larger((float)l[0], (float)l[1]));
+                norm = lm + log64(Lanes<L>::sum(exp64(l[0] - lm) + (a.K > L ? exp64(l[1] - lm) : 0.0)));
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (h == 1 && a.K <= 64) break;
+                if (h == 1 && a.K <= L) break;
                 if (!(z[h] <= kFloor)) e[h] = exp64(((double)z[h] - (double)M) * a.inv_t);
                 l[h] -= norm;
                 q[h] = exp64(l[h]);
             }
-            const double total = R + wave_sum2(e[0], e[1]), q_sum = wave_sum2(q[0], q[1]);
+            const double total = R + Lanes<L>::sum(e[0] + e[1]), q_sum = Lanes<L>::sum(q[0] + q[1]);
             const double ln_total = log64(total), per_total = 1.0 / total, per_S = 1.0 / S;
             bool dead = false;
             double terms = 0.0;
@@ -512,9 +572,9 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
             const bool has_rest = S > 0.0;
             const double q_rest = a.tail == ULORL_TAIL_BUCKET && has_rest && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
             const double mass = q_sum + q_rest;
-            double kl = wave_sum_f64(terms);
+            double kl = Lanes<L>::sum(terms);
             if (q_rest > 0.0) kl += q_rest * (log64(q_rest * per_S) - (((double)rest_max - (double)M) * a.inv_t - ln_total));
-            const bool ok = !__any(dead) && total > 0.0 && total < 1.0e300 && fabs(kl) < 1.0e300;
+            const bool ok = !Lanes<L>::any(dead) && total > 0.0 && total < 1.0e300 && fabs(kl) < 1.0e300;
             lse_out = total > 0.0 ? (float)((double)M * a.inv_t + ln_total) : __builtin_nanf("");
             if (ok) {
                 const double g = w * a.inv_D * a.inv_t;
@@ -538,7 +598,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (lane + 64 * h < a.K) top[lane + 64 * h] = grad[h];
+            if (lane + L * h < a.K) top[lane + L * h] = grad[h];
             // one call: the unlisted tokens' gradients are there already
             if (a.spin_limit > 0 && state == ROW_ON) store_top<Tr>(dlogits + row * a.row_stride, a.V, id[h], grad[h] * a.grad_out);
         }
@@ -550,34 +610,30 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
         }
     }
     if (a.spin_limit > 0 && a.flags[1] != 0u) {     // pieces whose workgroup waited in vain: their logits are whole, in place too
-        __threadfence();                            // the rows' results are this wave's own
+        __threadfence();                            // the rows' results are these lanes' own
         const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
-        for (int64_t row = (int64_t)blockIdx.x * NW + wave; row < a.N; row += (int64_t)gridDim.x * NW) {
+        for (int64_t row = (int64_t)blockIdx.x * ROWS + (int)threadIdx.x / L; row < a.N; row += (int64_t)gridDim.x * ROWS) {
             for (unsigned long long todo = a.pending[row]; todo != 0ull; todo &= todo - 1ull) {
                 const RestGradient rest(a.rest_coef[row] * a.grad_out, a.rest_max[row], a.scale);
                 const int begin = (__ffsll((long long)todo) - 1) * piece_vectors;
-                for (int i = begin + lane; i < min(all, begin + piece_vectors); i += 64)
+                for (int i = begin + lane; i < min(all, begin + piece_vectors); i += L)
                     store_vector<Tr>(dlogits + row * a.row_stride, a.V, i,
                                      rest.none ? u32x4{0u, 0u, 0u, 0u} : rest.template of<Tr>(load_vector<Tr>(logits + row * a.row_stride, a.V, i)));
             }
             if (a.pending[row] == 0ull) continue;
             __threadfence();                        // the listed tokens' again, over them
-            for (int j = lane; j < a.K; j += 64)
+            for (int j = lane; j < a.K; j += L)
                 store_top<Tr>(dlogits + row * a.row_stride, a.V, a.ids[row * a.K + j], a.top_grad[row * a.K + j] * a.grad_out);
         }
     }
-    if (lane == 0) part[wave] = mine;
+    // a row's first lane has what it contributed
+    const bool first = lane == 0;
+    if (!first) mine = Partial{0.0, 0, 0, 0, 0};
+    wave_partial(mine);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
-        Partial sum = {0.0, 0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            sum.loss += part[w].loss;
-            sum.on += part[w].on;
-            sum.weightless += part[w].weightless;
-            sum.empty += part[w].empty;
-            sum.status |= part[w].status;
-        }
+        const Partial sum = all_partials<NW>(part);
         Partial& to = a.partial[blockIdx.x];
         publish(&to.loss, sum.loss);
         publish(&to.on, sum.on);
@@ -596,26 +652,11 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
         q.empty += published(&from.empty);
         q.status |= published(&from.status);
     }
-    q.loss = wave_sum_f64(q.loss);
-    q.on = (int64_t)wave_sum_f64((double)q.on);                     // below 2^53: exact
-    q.weightless = (int64_t)wave_sum_f64((double)q.weightless);
-    q.empty = (int64_t)wave_sum_f64((double)q.empty);
-    int64_t status = 0;
-#pragma unroll
-    for (int bit = 1; bit <= ULORL_STATUS_BAD_TARGET; bit <<= 1) status |= __any((q.status & bit) != 0) ? bit : 0;
-    q.status = status;
-    if (lane == 0) part[wave] = q;
+    wave_partial(q);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = q;
     __syncthreads();
     if (threadIdx.x == 0) {
-        Partial sum = part[0];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            sum.loss += part[w].loss;
-            sum.on += part[w].on;
-            sum.weightless += part[w].weightless;
-            sum.empty += part[w].empty;
-            sum.status |= part[w].status;
-        }
+        const Partial sum = all_partials<NW>(part);
         *a.loss = (float)(sum.loss * a.inv_D);
         if (a.counters) {
             a.counters[0] = sum.on;
@@ -743,16 +784,27 @@ template <class Tr>
 int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const DistillArgs& a, hipStream_t st)
 {
     using elem = typename Tr::elem;
-    hipLaunchKernelGGL(distill_target_kernel, dim3((unsigned)((a.N + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
-    if (!launch_stream<Tr>(l, logits, dlogits, a, st)) return ULORL_ERR_HIP;
-    auto finish = [&](auto nt) {
-        constexpr int NT = decltype(nt)::value, NW = NT / 64;
-        const int64_t groups = (a.N + NW - 1) / NW;
-        hipLaunchKernelGGL((distill_finish_kernel<Tr, NT>), dim3((unsigned)(groups < kFinishGroups ? groups : kFinishGroups)), dim3(NT), 0, st,
-                           (const elem*)logits, (elem*)dlogits, (int32_t)(kThreads * l.shape.vpt), a);
+    const int L = lanes_of(a.K);
+    auto with_lanes = [&](const auto& f) {
+        if (L == 16) f(std::integral_constant<int, 16>{});
+        else if (L == 32) f(std::integral_constant<int, 32>{});
+        else f(std::integral_constant<int, 64>{});
     };
-    if (a.N <= (int64_t)kFinishGroups * (kFinishSmall / 64)) finish(std::integral_constant<int, kFinishSmall>{});
-    else finish(std::integral_constant<int, kFinishLarge>{});
+    auto groups = [&](int threads) { return (a.N * L + threads - 1) / threads; };
+    with_lanes([&](auto l_) {
+        hipLaunchKernelGGL((distill_target_kernel<decltype(l_)::value>), dim3((unsigned)groups(kThreads)), dim3(kThreads), 0, st, a);
+    });
+    if (!launch_stream<Tr>(l, logits, dlogits, a, st)) return ULORL_ERR_HIP;
+    with_lanes([&](auto l_) {
+        auto finish = [&](auto nt) {
+            constexpr int NT = decltype(nt)::value;
+            const int64_t n = groups(NT);
+            hipLaunchKernelGGL((distill_finish_kernel<Tr, NT, decltype(l_)::value>), dim3((unsigned)(n < kFinishGroups ? n : kFinishGroups)), dim3(NT), 0,
+                               st, (const elem*)logits, (elem*)dlogits, (int32_t)(kThreads * l.shape.vpt), a);
+        };
+        if (groups(kFinishSmall) <= kFinishGroups) finish(std::integral_constant<int, kFinishSmall>{});
+        else finish(std::integral_constant<int, kFinishLarge>{});
+    });
     if (dlogits != nullptr && a.spin_limit == 0) {
         launch_dense<Tr>(logits, a.N, a.V, a.row_stride, a.scale, a.rest_max, a.rest_coef, a.grad_out, nullptr, dlogits, st);
         launch_top<Tr>(a.N, a.V, a.row_stride, a.ids, a.K, a.top_grad, a.grad_out, nullptr, dlogits, st);
