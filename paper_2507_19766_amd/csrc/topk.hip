@@ -36,7 +36,10 @@ namespace {
 
 constexpr int kTopkThreads = 256;
 constexpr int kTopkWaves = kTopkThreads / 64;
-constexpr int kTopkUnroll = 8;
+// Vectors a thread has in flight: eight (four workgroups a compute unit) on rows of 256 KB and more, four (six workgroups) on
+// shorter ones, where the search is a larger part and more rows hide it.  us, eight / four: 4096 x 151936 bf16 201 / 203, 8192 x 64000
+// 181 / 173, 8000 x 32000 119 / 110, 20000 x 8192 141 / 110, 30000 x 2048 fp32 155 / 122.
+constexpr int kLongRow = 16384;       // vectors
 constexpr int kMaxK = 128;
 constexpr int kMaxGroups = 2560;      // group maxima of a row: 10 KB of LDS
 constexpr int kGroupsPerWave = 128;   // of the lists that a wave makes
@@ -407,10 +410,10 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
 // and the groups' maxima in sh.gmax, from begin's group on, valid after a barrier.
 // LG: log2 of the vectors in a group, or kManyVectors: a.lg, more than a run of 16 lanes.
 constexpr int kManyVectors = 5;
-template <class Tr, int LG>
+template <class Tr, int LG, int U>
 __device__ __forceinline__ Lane stream_vectors(const TopkArgs& a, const typename Tr::elem* rowp, int begin, int end, Shared& sh)
 {
-    constexpr int NT = kTopkThreads, U = kTopkUnroll, E = Tr::kPerVec;
+    constexpr int NT = kTopkThreads, E = Tr::kPerVec;
     const int tid = threadIdx.x;
     const int whole_end = min(a.V / E, end);        // where the whole vectors end
     const int g0 = begin >> a.lg;
@@ -510,7 +513,7 @@ __device__ __forceinline__ int64_t row_of_grid() { return (int64_t)blockIdx.y * 
 // One workgroup per row.  At 151936 bf16 logits and K 64 it reads 6.4 TB/s (the statistics alone: 7.0): its vector ALUs are
 // 85 % busy, the search adds 10 % of instructions (K 128: 25 %) and 7 us in which a workgroup loads little; four workgroups share a
 // compute unit (five, with registers in scratch memory for it, 20 % slower; 12 loads in flight instead of 8, three workgroups, 2 %).
-template <class Tr, int LG>
+template <class Tr, int LG, int U>
 __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
 {
     __shared__ Shared sh;
@@ -518,7 +521,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename T
     if (row >= a.N) return;
     const typename Tr::elem* rowp = logits + row * a.row_stride;
     const Token token = token_of<Tr>(a, rowp, row);
-    const Lane acc = stream_vectors<Tr, LG>(a, rowp, 0, (a.V + Tr::kPerVec - 1) / Tr::kPerVec, sh);
+    const Lane acc = stream_vectors<Tr, LG, U>(a, rowp, 0, (a.V + Tr::kPerVec - 1) / Tr::kPerVec, sh);
     const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
     finish_row<Tr>(a, rowp, row, st, token, sh);
 }
@@ -535,7 +538,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_piece_kernel(const typename
     const int64_t row = blockIdx.y;
     const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
     const int begin = (int)blockIdx.x * a.piece_vectors, end = min(all, begin + a.piece_vectors);
-    const Lane acc = stream_vectors<Tr, LG>(a, logits + row * a.row_stride, begin, end, sh);
+    const Lane acc = stream_vectors<Tr, LG, 4>(a, logits + row * a.row_stride, begin, end, sh);
     const Row st = merge_lanes(acc, a.scale, sh);
     RowParts& to = parts[row];
     if (threadIdx.x == 0) to.piece[blockIdx.x] = st;
@@ -600,14 +603,25 @@ void launch_topk(const void* logits, TopkArgs a, RowParts* parts, hipStream_t st
     if (parts != nullptr && a.N <= kSplitRows && batches >= kSplitBatches && pieces > 1 && ((int64_t)1 << a.lg) <= batch) {
         a.piece_vectors = (int32_t)(per * batch);
         with_group(a.lg, [&](auto lg) {
-            hipLaunchKernelGGL((topk_piece_kernel<Tr, decltype(lg)::value>), dim3((unsigned)pieces, (unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, parts);
+            constexpr int LG = decltype(lg)::value;
+            static_assert(kSplitBatches > 7 && 7 * 4 * kTopkThreads > (kMaxGroups << 1), "rows that are split have groups of four vectors or more");
+            if constexpr (LG >= 2)
+                hipLaunchKernelGGL((topk_piece_kernel<Tr, LG>), dim3((unsigned)pieces, (unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, parts);
         });
         hipLaunchKernelGGL((topk_merge_kernel<Tr>), dim3((unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, (int32_t)pieces, parts);
         return;
     }
     const dim3 grid((unsigned)(a.N < kRowsPerGridX ? a.N : kRowsPerGridX), (unsigned)((a.N + kRowsPerGridX - 1) / kRowsPerGridX));
     with_group(a.lg, [&](auto lg) {
-        hipLaunchKernelGGL((topk_row_kernel<Tr, decltype(lg)::value>), grid, dim3(kTopkThreads), 0, st, z, a);
+        constexpr int LG = decltype(lg)::value;
+        static_assert((kMaxGroups << 2) < kLongRow && kLongRow < (kMaxGroups << 3), "long rows have groups of eight vectors or more");
+        auto launch = [&](auto u) {
+            hipLaunchKernelGGL((topk_row_kernel<Tr, LG, decltype(u)::value>), grid, dim3(kTopkThreads), 0, st, z, a);
+        };
+        if constexpr (LG >= 4) launch(std::integral_constant<int, 8>{});
+        else if constexpr (LG < 3) launch(std::integral_constant<int, 4>{});
+        else if (all >= kLongRow) launch(std::integral_constant<int, 8>{});
+        else launch(std::integral_constant<int, 4>{});
     });
 }
 
