@@ -10,7 +10,7 @@
 // the listed probabilities would lose all its digits where the student is sure of them.  What a row is made of after that (K terms)
 // is in 64 bits: a divergence is a small sum of larger terms.
 //
-//   distill_target_kernel   is the target a distribution; what the row's gradient needs of it
+//   distill_target_kernel   is the target a distribution; what the row's gradient needs of it (rows of one piece: their own workgroups)
 //   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers, to (max, S); listed logits
 //   distill_row_kernel      one call: the same pieces, which tell each other their sums and write the gradient from the registers
 //   distill_finish_kernel   kl, the listed tokens' gradients, the unlisted ones' coefficient; the loss
@@ -125,6 +125,48 @@ inline int lanes_of(int K) { return K <= 32 ? 16 : K <= 64 ? 32 : 64; }
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
 
+// By L lanes, in each of them.
+template <int L>
+__device__ __forceinline__ RowTarget row_target(const DistillArgs& a, int64_t row, int lane)
+{
+    const float w = a.weights ? a.weights[row] : 1.0f;
+    int32_t id[2];
+    float l[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int j = lane + L * h;
+        id[h] = j < a.K ? a.ids[row * a.K + j] : -1;
+        l[h] = j < a.K ? a.teacher[row * a.K + j] : -INFINITY;
+        l[h] = id[h] >= 0 ? l[h] : -INFINITY;
+    }
+    RowTarget t = {0.0f, 0.0f, ROW_ON, 0};
+    if (w == 0.0f) {
+        t.state = ROW_WEIGHTLESS;
+        return t;
+    }
+    const bool beyond = id[0] >= a.V || id[1] >= a.V;
+    const bool bad = !finite(w) || !(l[0] <= 3.4028235e38f) || !(l[1] <= 3.4028235e38f);
+    if (Lanes<L>::any(beyond)) {
+        t.state = ROW_BAD_TOKEN;
+    } else if (Lanes<L>::any(bad)) {
+        t.state = ROW_BAD_TARGET;
+    } else if (!Lanes<L>::any(id[0] >= 0 || id[1] >= 0) || (a.tail == ULORL_TAIL_RENORM && !Lanes<L>::any(l[0] > -INFINITY || l[1] > -INFINITY))) {
+        t.state = ROW_EMPTY;
+    } else {
+        const double g = (double)w * a.inv_D * a.inv_t;
+        double mass = 1.0, rest = 0.0;
+        if (a.tail != ULORL_TAIL_RENORM) {
+            const double q = Lanes<L>::sum(exp64((double)l[0]) + (a.K > L ? exp64((double)l[1]) : 0.0));
+            rest = a.tail == ULORL_TAIL_BUCKET && q < 1.0 ? 1.0 - q : 0.0;
+            mass = q + rest;
+        }
+        t.mass = (float)(g * mass);
+        t.rest = (float)(g * rest);
+    }
+    return t;
+}
+
+// Rows of several pieces: what all of a row's workgroups have to know.
 template <int L>
 __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
 {
@@ -134,42 +176,9 @@ __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
     if (row >= a.N) return;
     if (a.spin_limit > 0) {         // the exchange of the one-call path starts from zeros
         if (lane == 0) a.pending[row] = 0ull;
-        if (a.C > 1)
-            for (int k = lane; k < 2 * a.C; k += L) a.slots[row * a.C * 2 + k] = 0ull;
+        for (int k = lane; k < 2 * a.C; k += L) a.slots[row * a.C * 2 + k] = 0ull;
     }
-    const float w = a.weights ? a.weights[row] : 1.0f;
-    int32_t id[2];
-    float l[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int j = lane + L * h;
-        id[h] = j < a.K ? a.ids[row * a.K + j] : -1;
-        l[h] = id[h] >= 0 ? a.teacher[row * a.K + j] : -INFINITY;
-    }
-    RowTarget t = {0.0f, 0.0f, ROW_ON, 0};
-    if (w == 0.0f) {
-        t.state = ROW_WEIGHTLESS;
-    } else {
-        const bool beyond = id[0] >= a.V || id[1] >= a.V;
-        const bool bad = !finite(w) || (id[0] >= 0 && !(l[0] <= 3.4028235e38f)) || (id[1] >= 0 && !(l[1] <= 3.4028235e38f));
-        if (Lanes<L>::any(beyond)) {
-            t.state = ROW_BAD_TOKEN;
-        } else if (Lanes<L>::any(bad)) {
-            t.state = ROW_BAD_TARGET;
-        } else if (!Lanes<L>::any(id[0] >= 0 || id[1] >= 0) || (a.tail == ULORL_TAIL_RENORM && !Lanes<L>::any(l[0] > -INFINITY || l[1] > -INFINITY))) {
-            t.state = ROW_EMPTY;
-        } else {
-            const double g = (double)w * a.inv_D * a.inv_t;
-            double mass = 1.0, rest = 0.0;
-            if (a.tail != ULORL_TAIL_RENORM) {
-                const double q = Lanes<L>::sum(exp64((double)l[0]) + (a.K > L ? exp64((double)l[1]) : 0.0));
-                rest = a.tail == ULORL_TAIL_BUCKET && q < 1.0 ? 1.0 - q : 0.0;
-                mass = q + rest;
-            }
-            t.mass = (float)(g * mass);
-            t.rest = (float)(g * rest);
-        }
-    }
+    const RowTarget t = row_target<L>(a, row, lane);
     if (lane == 0) a.target[row] = t;
 }
 
@@ -217,6 +226,8 @@ struct PieceShared {
     int32_t where[kMaxK];       // vector of the thread * 8 + element
     float m[kWaves], top_m[kWaves];
     double S[kWaves], top_S[kWaves];
+    RowTarget target;           // of a row of one piece
+    int32_t twice;
 };
 
 struct PieceSums {
@@ -224,27 +235,62 @@ struct PieceSums {
     double S, top_S;            // relative to them
 };
 
-// A row's piece c into registers (v) without its listed tokens, whose logits go to a.top_grad, and its sums (thread 0).  TOP: the listed
-// tokens' sum is wanted too.
-template <class Tr, int VPT, bool TOP>
-__device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT], PieceShared& sh)
+// A row's piece c into registers.
+template <class Tr, int VPT>
+__device__ __forceinline__ void load_piece(const typename Tr::elem* rowp, int32_t V, int c, u32x4 (&v)[VPT])
 {
-    constexpr int NT = kThreads, E = Tr::kPerVec;
-    const int tid = threadIdx.x, wave = tid >> 6;
-    const int nvec = a.V / E;
-    const int first = c * NT * VPT;
-    const int32_t id = tid < a.K ? a.ids[row * a.K + tid] : -1;
-    if (first + NT * VPT <= nvec) {
-        const char* const piece = reinterpret_cast<const char*>(rowp) + ((size_t)first << 4);
+    constexpr int NT = kThreads;
+    const int tid = threadIdx.x, first = c * NT * VPT;
+    if (first + NT * VPT <= V / Tr::kPerVec) {
+        const char* const piece = reinterpret_cast<const char*>(rowp) + ((size_t)first << 4);      // uniform base, lane offset
 #pragma unroll
         for (int k = 0; k < VPT; ++k) v[k] = load_stream(reinterpret_cast<const u32x4*>(piece + (size_t)k * NT * 16 + ((uint32_t)tid << 4)));
     } else {
 #pragma unroll
-        for (int k = 0; k < VPT; ++k) v[k] = load_vector<Tr>(rowp, a.V, first + k * NT + tid);
+        for (int k = 0; k < VPT; ++k) v[k] = load_vector<Tr>(rowp, V, first + k * NT + tid);
     }
+}
+
+// A row's target, and its piece c on the way into registers; false: the row does not count (and is not read where its weight is 0).
+// The workgroup of a row of one piece works the target out itself while the row is on its way, and no kernel runs before it.
+template <class Tr, int VPT>
+__device__ __forceinline__ bool start_piece(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT], RowTarget& target,
+                                            PieceShared& sh)
+{
+    if (a.C > 1) {
+        target = a.target[row];
+        if (target.state != ROW_ON) return false;
+        load_piece<Tr, VPT>(rowp, a.V, c, v);
+        return true;
+    }
+    const int tid = threadIdx.x;
+    if (a.weights == nullptr || a.weights[row] != 0.0f) load_piece<Tr, VPT>(rowp, a.V, c, v);
+    if (row == 0 && tid < 2) a.flags[tid] = 0u;         // for the kernel that follows
+    if (tid < 64) {
+        const RowTarget t = row_target<64>(a, row, tid);
+        if (tid == 0) sh.target = t;
+    }
+    __syncthreads();
+    target = sh.target;
+    if (target.state == ROW_ON) return true;
+    if (tid == 0) a.target[row] = target;
+    return false;
+}
+
+// A piece's registers (v) lose their listed tokens, whose logits go to a.top_grad; the piece's sums (thread 0).  TOP: the listed
+// tokens' sum is wanted too.
+template <class Tr, int VPT, bool TOP>
+__device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT],
+                                                const RowTarget& target, PieceShared& sh)
+{
+    constexpr int NT = kThreads, E = Tr::kPerVec;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int first = c * NT * VPT;
+    const int32_t id = tid < a.K ? a.ids[row * a.K + tid] : -1;
 
     // each thread's listed tokens as a chain in LDS
     sh.head[tid] = -1;
+    if (tid == 0) sh.twice = 0;
     __syncthreads();
     float z = kFloor;
     bool dead = false;                          // the row is no row: a token of the teacher's masked, or listed twice
@@ -262,7 +308,7 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
         for (int j = sh.head[at & (NT - 1)]; j >= 0; j = sh.next[j]) {
             if (j != tid && sh.where[j] == sh.where[tid]) {
                 dead = true;
-                a.target[row].twice = 1;
+                sh.twice = 1;
             }
         }
     }
@@ -297,6 +343,8 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
     __syncthreads();
     PieceSums p = {kFloor, kFloor, 0.0, 0.0};
     if (tid == 0) {
+        if (a.C == 1) a.target[row] = RowTarget{target.mass, target.rest, target.state, sh.twice};
+        else if (sh.twice != 0) a.target[row].twice = 1;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) p.m = larger(p.m, sh.m[w]);
 #pragma unroll
@@ -327,9 +375,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, kMo
 {
     __shared__ PieceShared sh;
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
-    if (row >= a.N || a.target[row].state != ROW_ON) return;
+    if (row >= a.N) return;
+    const typename Tr::elem* rowp = logits + row * a.row_stride;
     u32x4 v[VPT];
-    const PieceSums p = piece_sums<Tr, VPT, false>(a, logits + row * a.row_stride, row, (int)blockIdx.x, v, sh);
+    RowTarget target;
+    if (!start_piece<Tr, VPT>(a, rowp, row, (int)blockIdx.x, v, target, sh)) return;
+    const PieceSums p = piece_sums<Tr, VPT, false>(a, rowp, row, (int)blockIdx.x, v, target, sh);
     if (threadIdx.x == 0) {
         unsigned long long* slot = a.slots + (row * a.C + blockIdx.x) * 2;
         slot[0] = slot_word(p.m, p.S);
@@ -405,7 +456,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr
     typename Tr::elem* outp = dlogits + row * a.row_stride;
     char* const piece_out = reinterpret_cast<char*>(outp) + ((size_t)first << 4);
     const bool full = first + NT * VPT <= nvec;
-    const RowTarget target = a.target[row];
+    RowTarget target;
     u32x4 v[VPT];
     auto store_all = [&](const auto& value) {
 #pragma unroll
@@ -415,11 +466,12 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr
         }
     };
     const u32x4 zero = {0u, 0u, 0u, 0u};
-    if (target.state != ROW_ON) {
+    const typename Tr::elem* rowp = logits + row * a.row_stride;
+    if (!start_piece<Tr, VPT>(a, rowp, row, c, v, target, sh)) {
         store_all([&](int) { return zero; });
         return;
     }
-    const PieceSums p = piece_sums<Tr, VPT, true>(a, logits + row * a.row_stride, row, c, v, sh);
+    const PieceSums p = piece_sums<Tr, VPT, true>(a, rowp, row, c, v, target, sh);
     if (tid < 64) {
         unsigned long long* slot = a.slots + row * a.C * 2;
         unsigned long long w0 = slot_word(p.m, p.S), w1 = slot_word(p.top_m, p.top_S);
@@ -791,7 +843,7 @@ int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const Distil
         else f(std::integral_constant<int, 64>{});
     };
     auto groups = [&](int threads) { return (a.N * L + threads - 1) / threads; };
-    with_lanes([&](auto l_) {
+    if (a.C > 1) with_lanes([&](auto l_) {
         hipLaunchKernelGGL((distill_target_kernel<decltype(l_)::value>), dim3((unsigned)groups(kThreads)), dim3(kThreads), 0, st, a);
     });
     if (!launch_stream<Tr>(l, logits, dlogits, a, st)) return ULORL_ERR_HIP;
