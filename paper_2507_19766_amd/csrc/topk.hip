@@ -93,6 +93,7 @@ __device__ __forceinline__ void absorb_vectors(const u32x4 (&v)[U], float scale,
         a = before;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
+            if (!__any(!(vm[k] <= kFloor))) continue;        // all masked, most of a row under a grammar: nothing to add
             u32x4 again = v[k];
             asm volatile("" : "+v"(again));      // unpacked anew, instead of every logit being kept until here
             float g[E];
