@@ -349,15 +349,20 @@ int32_t ulorl_token_topk(
  *   counters [4] int64, may be NULL: rows that count, rows of weight 0, rows that list nothing (all entries missing;
  *                 RENORM: all of probability 0), status word
  * Rows that do not count (kl, gradient and lse are 0): weight 0; nothing listed; and with a status bit an id >= V
- * (ULORL_STATUS_BAD_TOKEN), an id twice, a log-prob that is not-a-number or +infinity, or a weight that is not finite
- * (ULORL_STATUS_BAD_TARGET).  A row that has not-a-number or +infinity among its logits, nothing unmasked, or a masked
+ * (ULORL_STATUS_BAD_TOKEN), an id twice, a log-prob that is not-a-number or +infinity, probabilities that sum to more
+ * than 1.25 (BUCKET, DROP: the values are no log-probs), or a weight that is not finite (ULORL_STATUS_BAD_TARGET).  A row that has not-a-number or +infinity among its logits, nothing unmasked, or a masked
  * token to which the teacher gives probability raises ULORL_STATUS_NONFINITE: kl and gradient 0, lse as it comes.
  *   workspace     >= ulorl_distill_workspace_bytes(N, V, dt) bytes, 256-byte aligned; need not be preserved.
  *
  * ulorl_distill_fwd      loss and per-row outputs; one read of the logits
  * ulorl_distill_bwd      dlogits from them; type and stride of logits, MAY BE THE SAME BUFFER.  grad_out: HOST scalar;
  *                        grad_scale: DEVICE scalar that multiplies it, or NULL
- * ulorl_distill_fwd_bwd  both
+ * ulorl_distill_fwd_bwd  both, with one read and one write of HBM per row: as in ulorl_token_loss_fwd_bwd a row is shared
+ *                        by workgroups that exchange their sums, with a bounded wait (what one that waited in vain left
+ *                        undone is written before the call's last kernel ends).  launch: HOST, may be NULL:
+ *                        ULORL_LAUNCH_PER_ROW takes the two calls' kernels instead (as rows beyond 64 pieces do: their
+ *                        gradient is that of the two calls bit for bit, otherwise to rounding), sync_spins bounds the
+ *                        wait; the rest is not looked at.
  */
 enum { ULORL_TAIL_BUCKET = 0, ULORL_TAIL_RENORM = 1, ULORL_TAIL_DROP = 2 };
 

@@ -43,6 +43,9 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kFinishGroups = 256;
 constexpr int kFinishSmall = 256, kFinishLarge = 1024;
 
+// Listed probabilities may sum to more than 1 by their rounding (log-probs kept in bf16: 2 %); beyond this they are no log-probs.
+constexpr double kMostMass = 1.25;
+
 enum { ROW_ON = 0, ROW_WEIGHTLESS = 1, ROW_EMPTY = 2, ROW_BAD_TOKEN = 3, ROW_BAD_TARGET = 4 };
 
 // What the stream has to know of a row's target: g Q and g q_rest, with g = weight / (D T).  twice: an id is listed twice, which the
@@ -157,6 +160,7 @@ __device__ __forceinline__ RowTarget row_target(const DistillArgs& a, int64_t ro
         double mass = 1.0, rest = 0.0;
         if (a.tail != ULORL_TAIL_RENORM) {
             const double q = Lanes<L>::sum(exp64((double)l[0]) + (a.K > L ? exp64((double)l[1]) : 0.0));
+            if (!(q <= kMostMass)) t.state = ROW_BAD_TARGET;
             rest = a.tail == ULORL_TAIL_BUCKET && q < 1.0 ? 1.0 - q : 0.0;
             mass = q + rest;
         }
