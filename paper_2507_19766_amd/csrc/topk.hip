@@ -34,25 +34,31 @@ using namespace ulorl_detail;
 
 namespace {
 
-constexpr int kTopkThreads = 256;
-constexpr int kTopkWaves = kTopkThreads / 64;
-// Vectors a thread has in flight: eight (four workgroups a compute unit) on rows of 256 KB and more, four (six workgroups) on
-// shorter ones, where the search is a larger part and more rows hide it.  us, eight / four: 4096 x 151936 bf16 201 / 203, 8192 x 64000
-// 181 / 173, 8000 x 32000 119 / 110, 20000 x 8192 141 / 110, 30000 x 2048 fp32 155 / 122.
+constexpr int kTopkThreads = 256;     // of a workgroup; 64 where a row is a wave's
+// Vectors a thread has in flight: eight (four workgroups a compute unit) on rows of 256 KB and more, four (seven workgroups) on
+// shorter ones, where the search is a larger part and more rows hide it.  us, eight / four with six workgroups: 4096 x 151936 bf16
+// 201 / 203, 8192 x 64000 181 / 173, 8000 x 32000 119 / 110; six / seven workgroups: 1777 x 32000 29.5 / 28.2, 20000 x 8192 112 / 106.
 constexpr int kLongRow = 16384;       // vectors
 constexpr int kMaxK = 128;
-constexpr int kMaxGroups = 2560;      // group maxima of a row: 10 KB of LDS
-constexpr int kGroupsPerWave = 128;   // of the lists that a wave makes
-constexpr int kElemsPerWave = 192;
-constexpr int kElemSlots = kElemsPerWave + 8;
+constexpr int kGroupsPerLane = 10;
+constexpr int max_groups(int nt) { return nt * kGroupsPerLane; }     // group maxima of a row: 10 KB of LDS with 256 threads
+constexpr int kMaxGroups = max_groups(kTopkThreads);
 constexpr uint32_t kOverflow = 0xffffffffu;
-static_assert(kMaxK <= kElemsPerWave && kMaxK <= kGroupsPerWave, "where a list overflows, K groups and K elements take its place");
 // Where rows are split: few of them, each long.  us, split / one workgroup a row: 1 row of 151936 bf16 12 / 16, fp32 12 / 25; 128 rows 20 / 23 and
 // 24 / 29; 256 rows 26 / 24 and 36 / 32; 1 row of 32000 bf16 11.5 / 9.1.
 constexpr int kMaxPieces = 64;
 constexpr int64_t kSplitRows = 160;
 constexpr int64_t kSplitBatches = 8;          // of 16 KB
 constexpr int64_t kFewWorkgroups = 1024;
+
+// Where one wave does a row: short rows, enough of them to fill the chip.  No barriers, and what a row costs besides its stream (joining
+// the lanes, the search) is done once instead of by four waves.  us with K 10, wave / workgroup of four: 20000 x 2048 fp32 37 / 84, 20000 x
+// 8192 bf16 64 / 106, 20000 x 16384 bf16 115 / 141, 4096 x 4096 fp32 16.5 / 21.5, 1024 x 4096 fp32 8.7 / 9.2; and where it is not taken,
+// 256 x 4096 fp32 8.0 / 6.4, 1024 x 16384 bf16 14.6 / 12.4, 20000 x 32000 bf16 (K 33) 226 / 226.  Rows as many as vectors in one, and
+// 1024, is where both are alike.
+constexpr int kWaveRow = 2048;        // vectors
+constexpr int64_t kManyRows = 1024;
+static_assert(kWaveRow <= (max_groups(64) << 2), "a wave's row has groups of four vectors at most");
 
 struct TopkArgs {
     const int32_t* token_ids;   // may be NULL
@@ -149,15 +155,21 @@ __device__ __forceinline__ uint32_t key_of_floor() { return ~__float_as_uint(kFl
 // Of equal logits the lower id is the larger key; 0: masked.
 __device__ __forceinline__ uint64_t ranked(uint32_t key, uint32_t id) { return key == 0u ? 0ull : ((uint64_t)key << 32) | (0xffffffffu - id); }
 
+template <int NT>
 struct Shared {
-    float gmax[kMaxGroups];
-    alignas(16) uint64_t elems[kTopkWaves * kElemSlots];
-    uint32_t groups[kTopkWaves * kGroupsPerWave];
-    double S[kTopkWaves], T[kTopkWaves];
-    float m[kTopkWaves];
-    uint32_t bound[kTopkWaves];
-    uint32_t counts[2][kTopkWaves];
-    uint32_t found[kTopkWaves];
+    static constexpr int kWaves = NT / 64;
+    static constexpr int kGroupsPerWave = kWaves == 1 ? 256 : 128;     // of the lists that a wave makes
+    static constexpr int kElemsPerWave = kWaves == 1 ? 288 : 192;
+    static constexpr int kElemSlots = kElemsPerWave + 8;
+    static_assert(kMaxK <= kElemsPerWave && kMaxK <= kGroupsPerWave, "where a list overflows, K groups and K elements take its place");
+    float gmax[max_groups(NT)];
+    alignas(16) uint64_t elems[kWaves * kElemSlots];
+    uint32_t groups[kWaves * kGroupsPerWave];
+    double S[kWaves], T[kWaves];
+    float m[kWaves];
+    uint32_t bound[kWaves];
+    uint32_t counts[2][kWaves];
+    uint32_t found[kWaves + 1];        // the second counter of a lone wave's exact search included
     double ln_s;                    // ln of the row's sum, by thread 0
 };
 
@@ -166,7 +178,8 @@ struct Row {
     float m;
     double S, T;
 };
-__device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared& sh)
+template <int NT>
+__device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared<NT>& sh)
 {
     const int wave = threadIdx.x >> 6;
     const float wm = wave_max(a.m);
@@ -186,9 +199,9 @@ __device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared& s
     __syncthreads();
     Row r = {sh.m[0], 0.0, 0.0};
 #pragma unroll
-    for (int w = 1; w < kTopkWaves; ++w) r.m = fmaxf(r.m, sh.m[w]);
+    for (int w = 1; w < NT / 64; ++w) r.m = fmaxf(r.m, sh.m[w]);
 #pragma unroll
-    for (int w = 0; w < kTopkWaves; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
         const float dw = (sh.m[w] - r.m) * scale;
         const double sw = (double)fast_exp2(dw);
         r.S += sw * sh.S[w];
@@ -198,28 +211,36 @@ __device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared& s
 }
 
 // Number of threads' items that hold, over the workgroup (uniform).  turn alternates, so that one barrier a call is enough.
-__device__ __forceinline__ uint32_t block_count(uint32_t mine, int turn, Shared& sh)
+template <int NT>
+__device__ __forceinline__ uint32_t block_count(uint32_t mine, int turn, Shared<NT>& sh)
 {
     double x = wave_sum_f64((double)mine);
     if ((threadIdx.x & 63) == 0) sh.counts[turn & 1][threadIdx.x >> 6] = (uint32_t)x;
     __syncthreads();
     uint32_t n = 0;
 #pragma unroll
-    for (int w = 0; w < kTopkWaves; ++w) n += sh.counts[turn & 1][w];
+    for (int w = 0; w < NT / 64; ++w) n += sh.counts[turn & 1][w];
     return n;
 }
 
-// The largest key that at least K of the ranked keys reach (0: there are fewer).  each(f) calls f(key) for every key of
-// this thread.
-template <class Each>
-__device__ uint64_t kth_ranked(const Each& each, uint32_t K, Shared& sh)
+// A key that exactly K of the ranked keys reach, all of them where there are fewer; ids are below n.  each(f) calls f(key) for every
+// key of this thread.  Of a key's lower half only the bits that ids differ in are looked for.
+template <int NT, class Each>
+__device__ uint64_t kth_ranked(const Each& each, uint32_t K, uint32_t n, Shared<NT>& sh)
 {
+    const int id_bits = 32 - __builtin_clz(n);
     uint64_t t = 0;
     for (int bit = 63; bit >= 0; --bit) {
+        if (bit < 32 && bit >= id_bits) {
+            t |= 1ull << bit;
+            continue;
+        }
         const uint64_t c = t | (1ull << bit);
         uint32_t mine = 0;
         each([&](uint64_t key) { mine += key >= c ? 1u : 0u; });
-        if (block_count(mine, bit, sh) >= K) t = c;
+        const uint32_t reach = block_count(mine, bit, sh);
+        if (reach >= K) t = c;
+        if (reach == K) break;
     }
     __syncthreads();
     return t;
@@ -271,31 +292,40 @@ __device__ __forceinline__ void each_element(const TopkArgs& a, const typename T
 // barrier; row is the same in all of them.  Each wave lists the groups and elements that are its own (neighbouring groups are
 // different waves'), so that two barriers are enough.  Cycles at 151936 logits, K 64, 2048 rows in flight: bound 2000, list 1000,
 // elements 4500, ranks 3000, of 85000 for the row.
-template <class Tr>
-__device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, Shared& sh)
+template <class Tr, int NT>
+__device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, Shared<NT>& sh)
 {
-    constexpr int E = Tr::kPerVec;
+    constexpr int E = Tr::kPerVec, W = NT / 64, kGroupsPerWave = Shared<NT>::kGroupsPerWave, kElemsPerWave = Shared<NT>::kElemsPerWave,
+                  kElemSlots = Shared<NT>::kElemSlots;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t K = (uint32_t)a.K;
-    const uint32_t per_wave = (K + kTopkWaves - 1) / kTopkWaves;
+    const uint32_t per_wave = (K + W - 1) / W;
     const int behind = (a.V / E) * E, tail = a.V - behind;       // elements behind the last whole vector
 
     // lower bound of the K-th largest
-    constexpr int kPerLane = kMaxGroups / kTopkThreads;
-    auto group_of = [&](int i) { return (i * 64 + lane) * kTopkWaves + wave; };
-    float mine[kPerLane];
-    float best = kFloor;
+    auto group_of = [&](int i) { return (i * 64 + lane) * W + wave; };
+    constexpr int P = 4 / W;            // of a lane's maxima this many take part: 256 over the workgroup, two times the largest K
+    float mine[kGroupsPerLane], best[P];
+    uint32_t best_key[P];
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) {
+    for (int p = 0; p < P; ++p) best[p] = kFloor;
+#pragma unroll
+    for (int i = 0; i < kGroupsPerLane; ++i) {
         mine[i] = group_of(i) < ngroups ? sh.gmax[group_of(i)] : kFloor;
-        best = larger(best, mine[i]);
+        best[i % P] = larger(best[i % P], mine[i]);
     }
-    const uint32_t best_key = key_of(best);
+#pragma unroll
+    for (int p = 0; p < P; ++p) best_key[p] = key_of(best[p]);
+    auto reach = [&](uint32_t c) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int p = 0; p < P; ++p) n += (uint32_t)__popcll(__ballot(best_key[p] >= c));
+        return n;
+    };
     uint32_t t = 0;
     for (int bit = 30; bit >= 0; bit -= 2) {        // two bits a step: the steps are a chain of scalar instructions
         const uint32_t c1 = t | (1u << bit), c2 = t | (2u << bit), c3 = t | (3u << bit);
-        const uint32_t n1 = (uint32_t)__popcll(__ballot(best_key >= c1)), n2 = (uint32_t)__popcll(__ballot(best_key >= c2)),
-                       n3 = (uint32_t)__popcll(__ballot(best_key >= c3));
+        const uint32_t n1 = reach(c1), n2 = reach(c2), n3 = reach(c3);
         const uint32_t n = n3 >= per_wave ? n3 : n2 >= per_wave ? n2 : n1;
         t = n3 >= per_wave ? c3 : n2 >= per_wave ? c2 : n1 >= per_wave ? c1 : t;
         if (n == per_wave) break;
@@ -303,7 +333,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     if (lane == 0) sh.bound[wave] = t;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kTopkWaves; ++w) t = min(t, sh.bound[w]);
+    for (int w = 0; w < W; ++w) t = min(t, sh.bound[w]);
     const float bound = value_of(max(t, key_of_floor() + 1u));
 
     // this wave's groups that reach it, and their elements that do
@@ -311,7 +341,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     uint64_t* elems = sh.elems + wave * kElemSlots;
     uint32_t n_groups = 0, n_elems = 0;         // uniform
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) {
+    for (int i = 0; i < kGroupsPerLane; ++i) {
         const uint64_t hits = __ballot(mine[i] >= bound);
         const uint32_t at = n_groups + hits_below(hits);
         if (mine[i] >= bound && at < kGroupsPerWave) groups[at] = (uint32_t)group_of(i);
@@ -333,37 +363,37 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     if (lane == 0) sh.found[wave] = overflow ? kOverflow : n_elems;
     if (!overflow && lane < 8) elems[n_elems + lane] = 0ull;        // the ranks are counted eight keys at a time
     __syncthreads();
-    uint32_t n[kTopkWaves];
+    uint32_t n[W];
     bool full = false;
 #pragma unroll
-    for (int w = 0; w < kTopkWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
         n[w] = sh.found[w];
         full = full || n[w] == kOverflow;
     }
     if (full) {     // uniform: the K-th largest key itself, of the groups and then of the elements of the K first groups
         const uint64_t tg = kth_ranked([&](const auto& f) {
-            for (int g = tid; g < ngroups; g += kTopkThreads) f(ranked(key_of(sh.gmax[g]), (uint32_t)g));
-        }, K, sh);
+            for (int g = tid; g < ngroups; g += NT) f(ranked(key_of(sh.gmax[g]), (uint32_t)g));
+        }, K, (uint32_t)ngroups, sh);
         if (tid == 0) sh.found[0] = sh.found[1] = 0;
         __syncthreads();
-        for (int g = tid; g < ngroups; g += kTopkThreads) {
+        for (int g = tid; g < ngroups; g += NT) {
             const uint64_t r = ranked(key_of(sh.gmax[g]), (uint32_t)g);
             if (r != 0ull && r >= tg) sh.groups[atomicAdd(&sh.found[0], 1u)] = (uint32_t)g;      // K at most: the keys differ
         }
         __syncthreads();
         const uint32_t listed = sh.found[0];
         auto each_key = [&](const auto& f) {
-            each_element<Tr>(a, rowp, sh.groups, listed, tid, kTopkThreads, [&](float x, uint32_t id) { f(ranked(key_of(x), id)); });
+            each_element<Tr>(a, rowp, sh.groups, listed, tid, NT, [&](float x, uint32_t id) { f(ranked(key_of(x), id)); });
             if (tid < tail) f(ranked(key_of(Tr::load1(rowp + behind + tid)), (uint32_t)(behind + tid)));
         };
-        const uint64_t te = kth_ranked(each_key, K, sh);
+        const uint64_t te = kth_ranked(each_key, K, (uint32_t)a.V, sh);
         each_key([&](uint64_t r) {
             if (r != 0ull && r >= te) sh.elems[atomicAdd(&sh.found[1], 1u)] = r;                    // K at most
         });
         __syncthreads();
         n[0] = sh.found[1];
 #pragma unroll
-        for (int w = 1; w < kTopkWaves; ++w) n[w] = 0;
+        for (int w = 1; w < W; ++w) n[w] = 0;
         if (tid < 8) sh.elems[n[0] + tid] = 0ull;
         __syncthreads();
     }
@@ -373,11 +403,11 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     float* logp = a.top_logp + row * a.K;
     uint32_t total = 0;
 #pragma unroll
-    for (int w = 0; w < kTopkWaves; ++w) total += n[w];
+    for (int w = 0; w < W; ++w) total += n[w];
     // a key's rank is its place; with few keys two or four lanes count for each
-    const uint32_t lg_parts = total <= kTopkThreads / 4 ? 2 : total <= kTopkThreads / 2 ? 1 : 0;
+    const uint32_t lg_parts = total <= NT / 4 ? 2 : total <= NT / 2 ? 1 : 0;
     const uint32_t part = (uint32_t)tid & ((1u << lg_parts) - 1u);
-    for (uint32_t j0 = 0; j0 < total; j0 += kTopkThreads >> lg_parts) {
+    for (uint32_t j0 = 0; j0 < total; j0 += NT >> lg_parts) {
         const uint32_t j = j0 + ((uint32_t)tid >> lg_parts);
         uint64_t key = 0;
         uint32_t at = j;
@@ -388,7 +418,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
         }
         uint32_t rank = 0;
 #pragma unroll
-        for (int w = 0; w < kTopkWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             for (uint32_t i = part * 8; i < n[w]; i += 8u << lg_parts) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) rank += sh.elems[w * kElemSlots + i + q] > key ? 1u : 0u;
@@ -401,7 +431,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
             logp[rank] = (float)(((double)value_of((uint32_t)(key >> 32)) - (double)st.m) * a.inv_t - ln_s);
         }
     }
-    for (uint32_t j = total + tid; j < K; j += kTopkThreads) {      // fewer unmasked tokens than were asked for
+    for (uint32_t j = total + tid; j < K; j += NT) {      // fewer unmasked tokens than were asked for
         ids[j] = -1;
         logp[j] = -INFINITY;
     }
@@ -411,10 +441,10 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
 // and the groups' maxima in sh.gmax, from begin's group on, valid after a barrier.
 // LG: log2 of the vectors in a group, or kManyVectors: a.lg, more than a run of 16 lanes.
 constexpr int kManyVectors = 5;
-template <class Tr, int LG, int U>
-__device__ __forceinline__ Lane stream_vectors(const TopkArgs& a, const typename Tr::elem* rowp, int begin, int end, Shared& sh)
+template <class Tr, int LG, int U, int NT>
+__device__ __forceinline__ Lane stream_vectors(const TopkArgs& a, const typename Tr::elem* rowp, int begin, int end, Shared<NT>& sh)
 {
-    constexpr int NT = kTopkThreads, E = Tr::kPerVec;
+    constexpr int E = Tr::kPerVec;
     const int tid = threadIdx.x;
     const int whole_end = min(a.V / E, end);        // where the whole vectors end
     const int g0 = begin >> a.lg;
@@ -422,7 +452,7 @@ __device__ __forceinline__ Lane stream_vectors(const TopkArgs& a, const typename
         for (int g = tid; g <= ((end - 1) >> a.lg) - g0; g += NT) sh.gmax[g] = kEmpty;
         __syncthreads();
     }
-    // the largest of each of this thread's four vectors, 256 apart from `first` on, into their groups'
+    // the largest of each of this thread's four vectors, NT apart from `first` on, into their groups'
     auto note = [&](const float (&vm)[4], int first, auto whole) {
         if constexpr (LG < 2) {
 #pragma unroll
@@ -483,8 +513,8 @@ __device__ __forceinline__ Token token_of(const TopkArgs& a, const typename Tr::
 }
 
 // A row's results from its statistics and its groups' maxima in sh.gmax.  All threads call it after a barrier.
-template <class Tr>
-__device__ __forceinline__ void finish_row(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, const Row& st, const Token& token, Shared& sh)
+template <class Tr, int NT>
+__device__ __forceinline__ void finish_row(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, const Row& st, const Token& token, Shared<NT>& sh)
 {
     constexpr int E = Tr::kPerVec;
     const int all = (a.V + E - 1) / E, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
@@ -498,13 +528,13 @@ __device__ __forceinline__ void finish_row(const TopkArgs& a, const typename Tr:
         if (a.logp) a.logp[row] = ok && token.has ? (float)(((double)token.z - (double)st.m) * a.inv_t - ln_s) : nan;
     }
     if (!ok) {
-        for (int j = threadIdx.x; j < a.K; j += kTopkThreads) {
+        for (int j = threadIdx.x; j < a.K; j += NT) {
             a.top_ids[row * a.K + j] = -1;
             a.top_logp[row * a.K + j] = __builtin_nanf("");
         }
         return;
     }
-    select_and_write<Tr>(a, rowp, row, ngroups, st, sh);
+    select_and_write<Tr, NT>(a, rowp, row, ngroups, st, sh);
 }
 
 // Rows over grid dimensions x and y: a launch holds at most 2^32 threads along one.
@@ -514,17 +544,17 @@ __device__ __forceinline__ int64_t row_of_grid() { return (int64_t)blockIdx.y * 
 // One workgroup per row.  At 151936 bf16 logits and K 64 it reads 6.4 TB/s (the statistics alone: 7.0): its vector ALUs are
 // 85 % busy, the search adds 10 % of instructions (K 128: 25 %) and 7 us in which a workgroup loads little; four workgroups share a
 // compute unit (five, with registers in scratch memory for it, 20 % slower; 12 loads in flight instead of 8, three workgroups, 2 %).
-template <class Tr, int LG, int U>
-__global__ __launch_bounds__(kTopkThreads) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
+template <class Tr, int LG, int U, int NT>
+__global__ __launch_bounds__(NT, U == 4 && NT == 256 ? 7 : 1) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
 {
-    __shared__ Shared sh;
+    __shared__ Shared<NT> sh;
     const int64_t row = row_of_grid();
     if (row >= a.N) return;
     const typename Tr::elem* rowp = logits + row * a.row_stride;
     const Token token = token_of<Tr>(a, rowp, row);
-    const Lane acc = stream_vectors<Tr, LG, U>(a, rowp, 0, (a.V + Tr::kPerVec - 1) / Tr::kPerVec, sh);
+    const Lane acc = stream_vectors<Tr, LG, U, NT>(a, rowp, 0, (a.V + Tr::kPerVec - 1) / Tr::kPerVec, sh);
     const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
-    finish_row<Tr>(a, rowp, row, st, token, sh);
+    finish_row<Tr, NT>(a, rowp, row, st, token, sh);
 }
 
 // Few rows: several workgroups stream a row's pieces, one more finishes it.  What a row's pieces leave for it:
@@ -535,11 +565,11 @@ struct RowParts {
 template <class Tr, int LG>
 __global__ __launch_bounds__(kTopkThreads) void topk_piece_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a, RowParts* parts)
 {
-    __shared__ Shared sh;
+    __shared__ Shared<kTopkThreads> sh;
     const int64_t row = blockIdx.y;
     const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
     const int begin = (int)blockIdx.x * a.piece_vectors, end = min(all, begin + a.piece_vectors);
-    const Lane acc = stream_vectors<Tr, LG, 4>(a, logits + row * a.row_stride, begin, end, sh);
+    const Lane acc = stream_vectors<Tr, LG, 4, kTopkThreads>(a, logits + row * a.row_stride, begin, end, sh);
     const Row st = merge_lanes(acc, a.scale, sh);
     RowParts& to = parts[row];
     if (threadIdx.x == 0) to.piece[blockIdx.x] = st;
@@ -549,7 +579,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_piece_kernel(const typename
 template <class Tr>
 __global__ __launch_bounds__(kTopkThreads) void topk_merge_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a, int32_t pieces, const RowParts* parts)
 {
-    __shared__ Shared sh;
+    __shared__ Shared<kTopkThreads> sh;
     __shared__ Row merged;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
@@ -572,7 +602,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_merge_kernel(const typename
     }
     __syncthreads();
     const Row st = merged;
-    finish_row<Tr>(a, rowp, row, st, token, sh);
+    finish_row<Tr, kTopkThreads>(a, rowp, row, st, token, sh);
 }
 
 // f(constant) for the log2 of a group's vectors.
@@ -613,11 +643,20 @@ void launch_topk(const void* logits, TopkArgs a, RowParts* parts, hipStream_t st
         return;
     }
     const dim3 grid((unsigned)(a.N < kRowsPerGridX ? a.N : kRowsPerGridX), (unsigned)((a.N + kRowsPerGridX - 1) / kRowsPerGridX));
+    if (all <= kWaveRow && a.N >= kManyRows && a.N >= all) {
+        a.lg = 0;
+        while (((all + ((int64_t)1 << a.lg) - 1) >> a.lg) > max_groups(64)) ++a.lg;
+        with_group(a.lg, [&](auto lg) {
+            constexpr int LG = decltype(lg)::value;
+            if constexpr (LG <= 2) hipLaunchKernelGGL((topk_row_kernel<Tr, LG, LG == 0 ? 4 : 8, 64>), grid, dim3(64), 0, st, z, a);
+        });
+        return;
+    }
     with_group(a.lg, [&](auto lg) {
         constexpr int LG = decltype(lg)::value;
         static_assert((kMaxGroups << 2) < kLongRow && kLongRow < (kMaxGroups << 3), "long rows have groups of eight vectors or more");
         auto launch = [&](auto u) {
-            hipLaunchKernelGGL((topk_row_kernel<Tr, LG, decltype(u)::value>), grid, dim3(kTopkThreads), 0, st, z, a);
+            hipLaunchKernelGGL((topk_row_kernel<Tr, LG, decltype(u)::value, kTopkThreads>), grid, dim3(kTopkThreads), 0, st, z, a);
         };
         if constexpr (LG >= 4) launch(std::integral_constant<int, 8>{});
         else if constexpr (LG < 3) launch(std::integral_constant<int, 4>{});

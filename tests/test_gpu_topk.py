@@ -13,10 +13,10 @@ EPS = 2.0 ** -23
 MASKED = -9e29
 
 
-def reference(z, k, T, y=None):
+def reference(z, k, T, y=None, lanes=256):
     """Everything in 64 bits, and how far 32-bit sums may be off.  A term e^x (x <= 0, relative to the maximum) is off by the
     rounding of its argument and one unit of the hardware's exp2, EPS (1 + |x|), and by up to eight roundings on its way
-    through the sums; the weighted sum is a chain of V / 256 fused steps per lane."""
+    through the sums; the weighted sum is a chain of V / lanes fused steps per lane."""
     z = z.double()
     z = torch.where(z <= MASKED, -math.inf, z)
     order = z.sort(dim=1, descending=True, stable=True)
@@ -30,7 +30,7 @@ def reference(z, k, T, y=None):
     ref = dict(lse=(m / T)[:, 0] + ln_s, entropy=ln_s + mean[:, 0])
     sums = (p * eta).sum(1)
     tol = dict(lse=sums + EPS * ref["lse"].abs(),
-               entropy=(p * eta * (1 + (X - mean).abs())).sum(1) + EPS * (ref["entropy"] + (z.shape[1] / 256 + 64) * mean[:, 0]))
+               entropy=(p * eta * (1 + (X - mean).abs())).sum(1) + EPS * (ref["entropy"] + (z.shape[1] / lanes + 64) * mean[:, 0]))
     n = min(k, z.shape[1])
     ids = torch.full((z.shape[0], k), -1, dtype=torch.int32, device=z.device)
     logp = torch.full((z.shape[0], k), -math.inf, dtype=torch.float64, device=z.device)
@@ -44,9 +44,9 @@ def reference(z, k, T, y=None):
     return ref, tol
 
 
-def check(z, k, T=1.0, y=None, **more):
+def check(z, k, T=1.0, y=None, lanes=256, **more):
     r = ulorl.token_topk(z, k, y, temperature=T, **more)
-    ref, tol = reference(z, k, T, y)
+    ref, tol = reference(z, k, T, y, lanes)
     wrong = (r.top_ids != ref["top_ids"]).any(1).nonzero()[:, 0]
     assert not len(wrong), (wrong[:5].tolist(), r.top_ids[wrong[0]].tolist()[:10], ref["top_ids"][wrong[0]].tolist()[:10])
     for name, t in tol.items():
@@ -111,6 +111,43 @@ def test_equal_logits_go_to_the_lower_id(V, k, dtype):
     z[8, V // 3:V // 3 + 64] = 20.0                             # ties within one neighbourhood
     z[9, -1] = z[9, 0] = 30.0
     check(z, k, 1.0, tokens(12, V))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [1, 2, 9, 64, 129, 1000, 1031, 2048, 2563, 5119, 8192, 8199, 16383, 16384, 16385])
+def test_many_short_rows(V, dtype):
+    n = max(1024, -(-V // (8 if dtype == BF else 4)))
+    for count, k, T in [(n, 1, 1.0), (n, 11, 0.7), (n + 1, 64, 1.0), (n - 1, 33, 1.0), (n, 128, 2.0)]:
+        check(rows(count, V, dtype, V + k), k, T, tokens(count, V, V), lanes=64)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [100, 1000, 4096, 8192])
+@pytest.mark.parametrize("k", [1, 8, 65, 128])
+def test_many_short_rows_with_ties_and_masks(V, k, dtype):
+    n = 2049
+    z = rows(n, V, dtype, k)
+    col = torch.arange(V, device=DEV)
+    z[0::16] = 1.5                                              # one value only
+    z[1::16] = (z[1::16] * 0.4).round()                         # a handful of values
+    z[2::16] = (col % 5).to(dtype)
+    z[3::16] = -(col // max(1, V // 3)).to(dtype)
+    z[4::16, ::3] = -0.0
+    z[5::16, V // 3:V // 3 + 64] = 20.0
+    z[6::16] = torch.linspace(-30, 30, V, device=DEV).to(dtype)
+    z[7::16] = torch.linspace(30, -30, V, device=DEV).to(dtype)
+    for at, value in [(8, -math.inf), (9, torch.finfo(dtype).min), (10, -1e30), (11, -math.inf)]:
+        left = (1, 7, 129, 40)[at - 8]
+        z[at::16] = torch.where(torch.rand(len(z[at::16]), V, device=DEV).argsort(1) < left, z[at::16], value)
+    y = z.argmax(1).int()
+    check(z, k, 1.0, y, lanes=64)
+    z[5], z[700, V // 2], z[2048, 0] = -math.inf, math.nan, math.inf
+    r = ulorl.token_topk(z, k, y)
+    bad = [5, 700, 2048]
+    assert (r.top_ids[bad] == -1).all() and all(getattr(r, name)[bad].isnan().all() for name in ("top_logp", "lse", "entropy", "logp"))
+    rest = torch.ones(n, dtype=torch.bool, device=DEV)
+    rest[bad] = False
+    assert torch.equal(r.top_ids[rest], reference(z[rest], k, 1.0)[0]["top_ids"])
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
