@@ -8,8 +8,9 @@
 //      vocabularies): the maximum of a vector is formed for the running maximum anyway, a group takes three lane
 //      permutations more.  The groups' maxima stay in LDS (at most kMaxGroups).
 //   2. A lower bound t of the K-th largest element: each wave finds the ceil(K / waves)-th largest of its lanes' largest
-//      group maxima by bisection over ballots; t is the smallest of the waves' values, so at least K groups reach t.
-//   3. Only groups that reach t (about 1.5 K of 2374) are read again, and their elements that reach t are listed: about as
+//      group maxima by bisection over ballots; t is the smallest of the waves' values, so at least K groups reach t.  (One bound
+//      over all lanes' maxima would leave 1.05 K groups at four times the ballots: no faster up to K 64, 5 % at 128.)
+//   3. Only groups that reach t (about 1.3 K of 2374 at K 64) are read again, and their elements that reach t are listed: about as
 //      many.  Each one's rank among them is its place in the answer.
 //
 // Ties: the order is by logit and then by the lower id, as one 64-bit key per element, so every rank is taken once.
@@ -290,8 +291,8 @@ __device__ __forceinline__ void each_element(const TopkArgs& a, const typename T
 
 // The K largest of a row whose groups' maxima are in sh.gmax, written in order.  All threads of the workgroup call it after a
 // barrier; row is the same in all of them.  Each wave lists the groups and elements that are its own (neighbouring groups are
-// different waves'), so that two barriers are enough.  Cycles at 151936 logits, K 64, 2048 rows in flight: bound 2000, list 1000,
-// elements 4500, ranks 3000, of 85000 for the row.
+// different waves'), so that two barriers are enough.  Cycles of a row at 2048 x 151936 bf16, K 64 (K 128): stream and
+// statistics 70000, bound 1900, list 1400, elements 7500 (13000), ranks and results 3100 (8300).
 template <class Tr, int NT>
 __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, Shared<NT>& sh)
 {
@@ -542,8 +543,9 @@ constexpr int64_t kRowsPerGridX = 1 << 20;
 __device__ __forceinline__ int64_t row_of_grid() { return (int64_t)blockIdx.y * kRowsPerGridX + blockIdx.x; }
 
 // One workgroup per row.  At 151936 bf16 logits and K 64 it reads 6.4 TB/s (the statistics alone: 7.0): its vector ALUs are
-// 85 % busy, the search adds 10 % of instructions (K 128: 25 %) and 7 us in which a workgroup loads little; four workgroups share a
+// 85 % busy, the search adds instructions (K 33: 7 %, K 128: 29 %) and 6 us in which a workgroup loads little; four workgroups share a
 // compute unit (five, with registers in scratch memory for it, 20 % slower; 12 loads in flight instead of 8, three workgroups, 2 %).
+// Short rows take 70 registers for seven (eight: scratch, 8000 x 32000 124 us instead of 104).
 template <class Tr, int LG, int U, int NT>
 __global__ __launch_bounds__(NT, U == 4 && NT == 256 ? 7 : 1) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
 {
