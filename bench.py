@@ -47,7 +47,7 @@ METRIC = "token-rows/sec fused fwd+bwd RL token loss (V=151936 bf16) + % HBM roo
 # expressed as measured / algorithmic ratios per row.  They hold for the kernel source they were taken
 # on: the digest below is checked at run time and `traffic` is null once the kernels changed.
 PMC = {
-    "source_sha256": "1eba5ac8739a94792f11e33212c68356cb26ba2e1b4ef3e6d88835735939c6fd",
+    "source_sha256": "702366601c1fd4aa9c4ffdfee79ac79bf89a3f8475ad2234194e83249da7c5fb",
     "fused_read": 1.0078, "fused_write": 1.0015,      # cluster_row_kernel: every row once, plus the polling of the exchange slots
     "bwd_read": 1.0007, "bwd_write": 1.0000,          # dlogits_chunk_kernel
 }
@@ -454,7 +454,7 @@ def main():
     bwd_gbs = bwd_bytes / (bwd_ms / K * 1e-3) / 1e9
     fwd_gbs = fwd_bytes / (fwd_ms / K * 1e-3) / 1e9
 
-    counters_valid = source_digest("token_loss.hip") == PMC["source_sha256"] and w.name == "cfg4_1x131072_bf16"
+    counters_valid = source_digest("token_loss.hip", "logits_stream.hpp") == PMC["source_sha256"] and w.name == "cfg4_1x131072_bf16"
     fused_traffic = (row_bytes * w.N * (PMC["fused_read"] + PMC["fused_write"]) if counters_valid else None)
     bwd_traffic = (row_bytes * (live * PMC["bwd_read"] + w.N * PMC["bwd_write"]) if counters_valid else None)
     headline_fused = args.path == "fused"
