@@ -11,7 +11,8 @@
 // is in 64 bits: a divergence is a small sum of larger terms.
 //
 //   distill_target_kernel   is the target a distribution; what the row's gradient needs of it (rows of one piece: their own workgroups)
-//   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers, to (max, S); listed logits
+//   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers (a short row a wave's), to (max, S);
+//                           listed logits
 //   distill_row_kernel      one call: the same pieces, which tell each other their sums and write the gradient from the registers
 //   distill_finish_kernel   kl, the listed tokens' gradients, the unlisted ones' coefficient; the loss
 //   distill_dense_kernel    the gradient of all tokens as if unlisted, one 16-byte vector per thread
@@ -35,13 +36,19 @@ namespace {
 
 constexpr int kMaxK = 128;              // two listed tokens per lane of a wave
 constexpr int64_t kMaxDistillRows = 1 << 24;
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kThreads = 256;           // of a workgroup; 64 where a row is a wave's
 // The finishing kernel takes no more workgroups than take their tickets quickly (2048 of them, 20 us; 256, 3):
 // small ones, spread over the chip, while 256 of them are enough (256 rows 7.5 us, in large ones 11.7), else large ones, which fill it
 // (8192 rows 27 us, in small ones 38).
 constexpr int kFinishGroups = 256;
 constexpr int kFinishSmall = 256, kFinishLarge = 1024;
+
+// Where one wave does a row: short rows, enough of them to fill the chip.  No barriers, and what a row costs besides its logits (target,
+// lists, joining the lanes) is done by one wave instead of four.  One call, K 8 (K 64), us, wave / workgroup of four: 16384 x 1000 bf16
+// 44 / 86 (53 / 97), 16384 x 4096 68 / 91 (90 / 110), 4096 x 2048 fp32 22 / 28 (30 / 36), 2048 x 4096 bf16 19 / 22 (24 / 25); and where it is
+// not taken, 1024 x 2048 fp32 15.4 / 15.4 (18.3 / 17.7), 16384 x 8192 bf16 113 / 107 (139 / 131).
+constexpr int64_t kWaveRow = 512;       // vectors
+constexpr int64_t kManyRows = 2048;
 
 // Listed probabilities may sum to more than 1 by their rounding (log-probs kept in bf16: 2 %); beyond this they are no log-probs.
 constexpr double kMostMass = 1.25;
@@ -224,8 +231,10 @@ __device__ __forceinline__ void absorb_rest(const u32x4 (&v)[VPT], float scale, 
     }
 }
 
+template <int NT>
 struct PieceShared {
-    int32_t head[kThreads];     // of a thread's listed tokens, -1: none
+    static constexpr int kWaves = NT / 64;
+    int32_t head[NT];           // of a thread's listed tokens, -1: none
     int32_t next[kMaxK];
     int32_t where[kMaxK];       // vector of the thread * 8 + element
     float m[kWaves], top_m[kWaves];
@@ -240,10 +249,9 @@ struct PieceSums {
 };
 
 // A row's piece c into registers.
-template <class Tr, int VPT>
+template <class Tr, int VPT, int NT>
 __device__ __forceinline__ void load_piece(const typename Tr::elem* rowp, int32_t V, int c, u32x4 (&v)[VPT])
 {
-    constexpr int NT = kThreads;
     const int tid = threadIdx.x, first = c * NT * VPT;
     if (first + NT * VPT <= V / Tr::kPerVec) {
         const char* const piece = reinterpret_cast<const char*>(rowp) + ((size_t)first << 4);      // uniform base, lane offset
@@ -257,18 +265,18 @@ __device__ __forceinline__ void load_piece(const typename Tr::elem* rowp, int32_
 
 // A row's target, and its piece c on the way into registers; false: the row does not count (and is not read where its weight is 0).
 // The workgroup of a row of one piece works the target out itself while the row is on its way, and no kernel runs before it.
-template <class Tr, int VPT>
+template <class Tr, int VPT, int NT>
 __device__ __forceinline__ bool start_piece(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT], RowTarget& target,
-                                            PieceShared& sh)
+                                            PieceShared<NT>& sh)
 {
     if (a.C > 1) {
         target = a.target[row];
         if (target.state != ROW_ON) return false;
-        load_piece<Tr, VPT>(rowp, a.V, c, v);
+        load_piece<Tr, VPT, NT>(rowp, a.V, c, v);
         return true;
     }
     const int tid = threadIdx.x;
-    if (a.weights == nullptr || a.weights[row] != 0.0f) load_piece<Tr, VPT>(rowp, a.V, c, v);
+    if (a.weights == nullptr || a.weights[row] != 0.0f) load_piece<Tr, VPT, NT>(rowp, a.V, c, v);
     if (row == 0 && tid < 2) a.flags[tid] = 0u;         // for the kernel that follows
     if (tid < 64) {
         const RowTarget t = row_target<64>(a, row, tid);
@@ -283,35 +291,47 @@ __device__ __forceinline__ bool start_piece(const DistillArgs& a, const typename
 
 // A piece's registers (v) lose their listed tokens, whose logits go to a.top_grad; the piece's sums (thread 0).  TOP: the listed
 // tokens' sum is wanted too.
-template <class Tr, int VPT, bool TOP>
+template <class Tr, int VPT, bool TOP, int NT>
 __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT],
-                                                const RowTarget& target, PieceShared& sh)
+                                                const RowTarget& target, PieceShared<NT>& sh)
 {
-    constexpr int NT = kThreads, E = Tr::kPerVec;
+    constexpr int E = Tr::kPerVec, kWaves = NT / 64;
+    constexpr int H = NT < kMaxK ? kMaxK / NT : 1;          // listed tokens a thread
     const int tid = threadIdx.x, wave = tid >> 6;
     const int first = c * NT * VPT;
-    const int32_t id = tid < a.K ? a.ids[row * a.K + tid] : -1;
+    int32_t id[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) id[h] = tid + h * NT < a.K ? a.ids[row * a.K + tid + h * NT] : -1;
 
     // each thread's listed tokens as a chain in LDS
     sh.head[tid] = -1;
     if (tid == 0) sh.twice = 0;
     __syncthreads();
-    float z = kFloor;
-    bool dead = false;                          // the row is no row: a token of the teacher's masked, or listed twice
-    const int at = id / E - first;              // id < V: the row's state says so
-    const bool in_piece = id >= 0 && at >= 0 && at < NT * VPT;
-    if (in_piece) {
-        z = Tr::load1(rowp + id);
-        a.top_grad[row * a.K + tid] = z;
-        sh.where[tid] = (at / NT) * 8 + (id & (E - 1));
-        sh.next[tid] = atomicExch(&sh.head[at & (NT - 1)], tid);
-        dead = z <= kFloor && a.teacher[row * a.K + tid] > -INFINITY;
+    float z[H];
+    bool dead[H], in_piece[H];                  // dead: the row is no row, a token of the teacher's masked, or listed twice
+    int at[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const int j = tid + h * NT;
+        z[h] = kFloor;
+        dead[h] = false;
+        at[h] = id[h] / E - first;              // id < V: the row's state says so
+        in_piece[h] = id[h] >= 0 && at[h] >= 0 && at[h] < NT * VPT;
+        if (in_piece[h]) {
+            z[h] = Tr::load1(rowp + id[h]);
+            a.top_grad[row * a.K + j] = z[h];
+            sh.where[j] = (at[h] / NT) * 8 + (id[h] & (E - 1));
+            sh.next[j] = atomicExch(&sh.head[at[h] & (NT - 1)], j);
+            dead[h] = z[h] <= kFloor && a.teacher[row * a.K + j] > -INFINITY;
+        }
     }
     __syncthreads();
-    if (in_piece) {
-        for (int j = sh.head[at & (NT - 1)]; j >= 0; j = sh.next[j]) {
-            if (j != tid && sh.where[j] == sh.where[tid]) {
-                dead = true;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        if (!in_piece[h]) continue;
+        for (int j = sh.head[at[h] & (NT - 1)]; j >= 0; j = sh.next[j]) {
+            if (j != tid + h * NT && sh.where[j] == sh.where[tid + h * NT]) {
+                dead[h] = true;
                 sh.twice = 1;
             }
         }
@@ -335,9 +355,15 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
         sh.S[wave] = wS;
     }
     if constexpr (TOP) {
-        const float wt = wave_max(z);
-        double top = z > kFloor ? (double)fast_exp2((z - wt) * a.scale) : 0.0;
-        if (z != z || dead) top = (double)__builtin_nanf("");
+        float mine = z[0];
+        if constexpr (H > 1) mine = larger(mine, z[1]);
+        const float wt = wave_max(mine);
+        double top = 0.0;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            if (z[h] > kFloor) top += (double)fast_exp2((z[h] - wt) * a.scale);
+            if (z[h] != z[h] || dead[h]) top = (double)__builtin_nanf("");
+        }
         top = wave_sum_f64(top);
         if ((tid & 63) == 0) {
             sh.top_m[wave] = wt;
@@ -374,17 +400,17 @@ __device__ __forceinline__ unsigned long long slot_word(float m, double S)
 template <class Tr, int VPT>
 constexpr int kMostWaves = Tr::kPerVec == 8 && VPT >= 11 ? 4 : 8;
 
-template <class Tr, int VPT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, kMostWaves<Tr, VPT>))) void distill_piece_kernel(const typename Tr::elem* logits, DistillArgs a)
+template <class Tr, int VPT, int NT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(1, kMostWaves<Tr, VPT>))) void distill_piece_kernel(const typename Tr::elem* logits, DistillArgs a)
 {
-    __shared__ PieceShared sh;
+    __shared__ PieceShared<NT> sh;
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
     if (row >= a.N) return;
     const typename Tr::elem* rowp = logits + row * a.row_stride;
     u32x4 v[VPT];
     RowTarget target;
-    if (!start_piece<Tr, VPT>(a, rowp, row, (int)blockIdx.x, v, target, sh)) return;
-    const PieceSums p = piece_sums<Tr, VPT, false>(a, rowp, row, (int)blockIdx.x, v, target, sh);
+    if (!start_piece<Tr, VPT, NT>(a, rowp, row, (int)blockIdx.x, v, target, sh)) return;
+    const PieceSums p = piece_sums<Tr, VPT, false, NT>(a, rowp, row, (int)blockIdx.x, v, target, sh);
     if (threadIdx.x == 0) {
         unsigned long long* slot = a.slots + (row * a.C + blockIdx.x) * 2;
         slot[0] = slot_word(p.m, p.S);
@@ -446,11 +472,10 @@ __device__ __forceinline__ void store_top(typename Tr::elem* outp, int32_t V, in
 // A row's pieces are neighbours in dispatch order, so partners are resident or next in line; the wait is bounded all the same: a
 // workgroup whose wait expires writes nothing (in place, its logits stay) and marks its piece, which distill_finish_kernel then
 // writes.
-template <class Tr, int VPT>
-__global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, DistillArgs a)
+template <class Tr, int VPT, int NT>
+__global__ __launch_bounds__(NT) void distill_row_kernel(const typename Tr::elem* logits, typename Tr::elem* dlogits, DistillArgs a)
 {
-    constexpr int NT = kThreads;
-    __shared__ PieceShared sh;
+    __shared__ PieceShared<NT> sh;
     __shared__ float bc_coef, bc_max;
     __shared__ int bc_expired;
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
@@ -471,11 +496,11 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(const typename Tr
     };
     const u32x4 zero = {0u, 0u, 0u, 0u};
     const typename Tr::elem* rowp = logits + row * a.row_stride;
-    if (!start_piece<Tr, VPT>(a, rowp, row, c, v, target, sh)) {
+    if (!start_piece<Tr, VPT, NT>(a, rowp, row, c, v, target, sh)) {
         store_all([&](int) { return zero; });
         return;
     }
-    const PieceSums p = piece_sums<Tr, VPT, true>(a, rowp, row, c, v, target, sh);
+    const PieceSums p = piece_sums<Tr, VPT, true, NT>(a, rowp, row, c, v, target, sh);
     if (tid < 64) {
         unsigned long long* slot = a.slots + row * a.C * 2;
         unsigned long long w0 = slot_word(p.m, p.S), w1 = slot_word(p.top_m, p.top_S);
@@ -757,6 +782,7 @@ __global__ __launch_bounds__(kThreads) void distill_top_kernel(const int32_t* id
 struct Layout {
     size_t target, partial, flags, pending, slots, total;
     ClusterShape shape;         // vectors per thread, pieces per row
+    int threads;                // of a piece's workgroup
     bool cooperative;           // a wave can poll a row's pieces
 };
 
@@ -765,6 +791,11 @@ Layout layout_of(int64_t N, int64_t V, int32_t dt)
     Layout l;
     const int64_t E = dt == ULORL_F32 ? 4 : 8, all = (V + E - 1) / E;
     l.shape = cluster_shape(all * E, dt);
+    l.threads = kThreads;
+    if (all <= kWaveRow && N >= kManyRows) {
+        l.threads = 64;
+        l.shape = ClusterShape{all <= kWaveRow / 2 ? 4 : 8, 1};
+    }
     l.cooperative = l.shape.pieces > 0;
     if (l.shape.pieces == 0) {                      // more than 64 pieces: no limit to the two-pass path
         l.shape.vpt = 15;
@@ -799,19 +830,22 @@ bool launch_stream(const Layout& l, const void* logits, void* dlogits, const Dis
     using elem = typename Tr::elem;
     // x: piece (fastest, so a row's pieces have consecutive linear ids), y/z: row
     const dim3 grid = rows_grid((unsigned)a.C, a.N);
-#define ULORL_CASE(VPT_)                                                                                                                   \
-    if (l.shape.vpt == VPT_) {                                                                                                             \
-        if (a.spin_limit > 0)                                                                                                              \
-            hipLaunchKernelGGL((distill_row_kernel<Tr, VPT_>), grid, dim3(kThreads), 0, st, (const elem*)logits, (elem*)dlogits, a);       \
-        else                                                                                                                               \
-            hipLaunchKernelGGL((distill_piece_kernel<Tr, VPT_>), grid, dim3(kThreads), 0, st, (const elem*)logits, a);                     \
-        return true;                                                                                                                       \
-    }
-    ULORL_CASE(4) ULORL_CASE(8) ULORL_CASE(13) ULORL_CASE(15)
+    auto launch = [&](auto vpt, auto nt) {
+        constexpr int VPT = decltype(vpt)::value, NT = decltype(nt)::value;
+        if (a.spin_limit > 0)
+            hipLaunchKernelGGL((distill_row_kernel<Tr, VPT, NT>), grid, dim3(NT), 0, st, (const elem*)logits, (elem*)dlogits, a);
+        else
+            hipLaunchKernelGGL((distill_piece_kernel<Tr, VPT, NT>), grid, dim3(NT), 0, st, (const elem*)logits, a);
+        return true;
+    };
+#define ULORL_CASE(VPT_, NT_) \
+    if (l.shape.vpt == VPT_ && l.threads == NT_) return launch(std::integral_constant<int, VPT_>{}, std::integral_constant<int, NT_>{});
+    ULORL_CASE(4, 64) ULORL_CASE(8, 64)
+    ULORL_CASE(4, kThreads) ULORL_CASE(8, kThreads) ULORL_CASE(13, kThreads) ULORL_CASE(15, kThreads)
     if constexpr (Tr::kPerVec == 8) {
-        ULORL_CASE(6) ULORL_CASE(7) ULORL_CASE(11)
+        ULORL_CASE(6, kThreads) ULORL_CASE(7, kThreads) ULORL_CASE(11, kThreads)
     } else {
-        ULORL_CASE(20)
+        ULORL_CASE(20, kThreads)
     }
 #undef ULORL_CASE
     return false;
@@ -856,7 +890,7 @@ int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const Distil
             constexpr int NT = decltype(nt)::value;
             const int64_t n = groups(NT);
             hipLaunchKernelGGL((distill_finish_kernel<Tr, NT, decltype(l_)::value>), dim3((unsigned)(n < kFinishGroups ? n : kFinishGroups)), dim3(NT), 0,
-                               st, (const elem*)logits, (elem*)dlogits, (int32_t)(kThreads * l.shape.vpt), a);
+                               st, (const elem*)logits, (elem*)dlogits, (int32_t)(l.threads * l.shape.vpt), a);
         };
         if (groups(kFinishSmall) <= kFinishGroups) finish(std::integral_constant<int, kFinishSmall>{});
         else finish(std::integral_constant<int, kFinishLarge>{});

@@ -183,6 +183,50 @@ def test_large_vocabularies(n, V, K, dtype):
     check(z, ids, logp, w, ulorl.DistillParams())
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [1, 7, 129, 1000, 1024, 1025, 2047, 2048, 2049, 4096, 4097])
+def test_many_short_rows(V, dtype):
+    for n, K, tail in [(2047, 9, ulorl.TAIL_BUCKET), (2048, 64, ulorl.TAIL_BUCKET), (2049, 65, ulorl.TAIL_DROP), (2500, 128, ulorl.TAIL_RENORM)]:
+        z, ids, logp, w = problem(n, V, K, dtype, V + K, ragged=True, tail=tail)
+        w[n // 2], w[n - 1] = 0.0, 0.0
+        check(z, ids, logp, w, ulorl.DistillParams(tail=tail), ("one", "two"))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [600, 2000, 4096])
+def test_many_short_rows_that_do_not_count(V, dtype):
+    n, K = 2050, 100
+    z, ids, logp, w = problem(n, V, K, dtype, 1)
+    w = w.abs() + 0.1
+    z[1, 17] = math.nan
+    z[20, ids[20, 4].long()] = math.nan
+    z[300, V - 1] = math.inf
+    z[401, ids[401, 99].long()] = math.inf
+    z[555] = -math.inf
+    z[666, ids[666, 70].long()] = -math.inf                     # masked, and the teacher wants it
+    ids[777, 2] = V
+    ids[888, 3] = ids[888, 67]                                  # an id twice, and by the same thread of a wave
+    ids[889, 99] = ids[889, 98]
+    ids[2049, 64] = ids[2049, 0]
+    logp[1000, 5] = math.nan
+    w[1200] = math.nan
+    w[2000] = 0.0
+    z[2000], ids[2000], logp[2000] = math.nan, V + 5, math.nan  # padding: not looked at
+    bad = [1, 20, 300, 401, 555, 666, 777, 888, 889, 2049, 1000, 1200, 2000]
+    good = torch.ones(n, dtype=torch.bool, device=DEV)
+    good[bad] = False
+    ref, tol = reference(z[good], ids[good], logp[good], w[good], ulorl.DistillParams(denominator=n))
+    def look(r, d):
+        assert r.counters.tolist() == [n - len(bad), 1, 0, 1 | 2 | 16]
+        assert (r.kl[bad] == 0).all() and (d[bad] == 0).all() and (r.top_grad[bad] == 0).all() and (r.rest_coef[bad] == 0).all()
+        compare(dict(kl=r.kl[good], lse=r.lse[good], loss=r.loss, dlogits=d[good]), ref, tol, dtype)
+    p = ulorl.DistillParams()
+    look(*ulorl.distill_fwd_bwd(z, ids, logp, w, p))
+    r = ulorl.distill_fwd(z, ids, logp, w, p)
+    look(r, ulorl.distill_bwd(z, ids, r, p))
+    look(*ulorl.distill_fwd_bwd(z, ids, logp, w, p, inplace=True))
+
+
 @pytest.mark.parametrize("n", [2, 3, 4, 5, 63, 257, 4095, 4097, 20001])
 def test_numbers_of_rows(n):
     z, ids, logp, w = problem(n, 1003, 9, BF, n)
