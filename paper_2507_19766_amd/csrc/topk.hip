@@ -41,12 +41,15 @@ constexpr int kTopkThreads = 256;     // of a workgroup; 64 where a row is a wav
 // 201 / 203, 8192 x 64000 181 / 173, 8000 x 32000 119 / 110; six / seven workgroups: 1777 x 32000 29.5 / 28.2, 20000 x 8192 112 / 106.
 constexpr int kLongRow = 16384;       // vectors
 constexpr int kMaxK = 128;
-constexpr int kGroupsPerLane = 10;
-constexpr int max_groups(int nt) { return nt * kGroupsPerLane; }     // group maxima of a row: 10 KB of LDS with 256 threads
-constexpr int kMaxGroups = max_groups(kTopkThreads);
+constexpr int groups_per_lane(int nt) { return nt <= 256 ? 10 : 2560 / nt; }
+constexpr int max_groups(int nt) { return nt * groups_per_lane(nt); }     // group maxima of a row: 10 KB of LDS with 256 threads
+constexpr int kMaxGroups = max_groups(kTopkThreads);                  // and of a split row's, with 512
 constexpr uint32_t kOverflow = 0xffffffffu;
 // Where rows are split: few of them, each long.  us, split / one workgroup a row: 1 row of 151936 bf16 12 / 16, fp32 12 / 25; 128 rows 20 / 23 and
 // 24 / 29; 256 rows 26 / 24 and 36 / 32; 1 row of 32000 bf16 11.5 / 9.1.
+// Of the workgroup that finishes a split row, whose chain of steps is what such a call waits for.  us with 256 / 512 / 1024, K 20 (K 128):
+// 1 row of 151936 bf16 11.5 / 10.9 / 13.2 (17 / 14 / 16), 64 rows 15.1 / 15.1 / 17.0 (28 / 20.5 / 20.2).
+constexpr int kMergeThreads = 512;
 constexpr int kMaxPieces = 64;
 constexpr int64_t kSplitRows = 160;
 constexpr int64_t kSplitBatches = 8;          // of 16 KB
@@ -297,7 +300,7 @@ template <class Tr, int NT>
 __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, int ngroups, const Row& st, Shared<NT>& sh)
 {
     constexpr int E = Tr::kPerVec, W = NT / 64, kGroupsPerWave = Shared<NT>::kGroupsPerWave, kElemsPerWave = Shared<NT>::kElemsPerWave,
-                  kElemSlots = Shared<NT>::kElemSlots;
+                  kElemSlots = Shared<NT>::kElemSlots, kGroupsPerLane = groups_per_lane(NT);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t K = (uint32_t)a.K;
     const uint32_t per_wave = (K + W - 1) / W;
@@ -305,7 +308,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
 
     // lower bound of the K-th largest
     auto group_of = [&](int i) { return (i * 64 + lane) * W + wave; };
-    constexpr int P = 4 / W;            // of a lane's maxima this many take part: 256 over the workgroup, two times the largest K
+    constexpr int P = W < 4 ? 4 / W : 1;            // of a lane's maxima this many take part: 256 over the workgroup at least, two times the largest K
     float mine[kGroupsPerLane], best[P];
     uint32_t best_key[P];
 #pragma unroll
@@ -579,9 +582,9 @@ __global__ __launch_bounds__(kTopkThreads) void topk_piece_kernel(const typename
     for (int g = g0 + (int)threadIdx.x; g <= g1; g += kTopkThreads) to.gmax[g] = sh.gmax[g - g0];
 }
 template <class Tr>
-__global__ __launch_bounds__(kTopkThreads) void topk_merge_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a, int32_t pieces, const RowParts* parts)
+__global__ __launch_bounds__(kMergeThreads) void topk_merge_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a, int32_t pieces, const RowParts* parts)
 {
-    __shared__ Shared<kTopkThreads> sh;
+    __shared__ Shared<kMergeThreads> sh;
     __shared__ Row merged;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
@@ -590,10 +593,10 @@ __global__ __launch_bounds__(kTopkThreads) void topk_merge_kernel(const typename
     const Token token = token_of<Tr>(a, rowp, row);
     const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
 #pragma unroll
-    for (int i = 0; i < kMaxGroups / kTopkThreads; ++i)
-        if (i * kTopkThreads + tid < ngroups) sh.gmax[i * kTopkThreads + tid] = from.gmax[i * kTopkThreads + tid];
+    for (int i = 0; i < groups_per_lane(kMergeThreads); ++i)
+        if (i * kMergeThreads + tid < ngroups) sh.gmax[i * kMergeThreads + tid] = from.gmax[i * kMergeThreads + tid];
     if (tid < 64) {         // a piece per lane
-        static_assert(kMaxPieces == 64, "one piece per lane");
+        static_assert(kMaxPieces == 64 && max_groups(kMergeThreads) == kMaxGroups, "one piece per lane; the pieces' groups");
         Row p = {kFloor, 0.0, 0.0};
         if (tid < pieces) p = from.piece[tid];
         const float m = wave_max(p.m);
@@ -604,7 +607,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_merge_kernel(const typename
     }
     __syncthreads();
     const Row st = merged;
-    finish_row<Tr, kTopkThreads>(a, rowp, row, st, token, sh);
+    finish_row<Tr, kMergeThreads>(a, rowp, row, st, token, sh);
 }
 
 // f(constant) for the log2 of a group's vectors.
@@ -641,7 +644,7 @@ void launch_topk(const void* logits, TopkArgs a, RowParts* parts, hipStream_t st
             if constexpr (LG >= 2)
                 hipLaunchKernelGGL((topk_piece_kernel<Tr, LG>), dim3((unsigned)pieces, (unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, parts);
         });
-        hipLaunchKernelGGL((topk_merge_kernel<Tr>), dim3((unsigned)a.N), dim3(kTopkThreads), 0, st, z, a, (int32_t)pieces, parts);
+        hipLaunchKernelGGL((topk_merge_kernel<Tr>), dim3((unsigned)a.N), dim3(kMergeThreads), 0, st, z, a, (int32_t)pieces, parts);
         return;
     }
     const dim3 grid((unsigned)(a.N < kRowsPerGridX ? a.N : kRowsPerGridX), (unsigned)((a.N + kRowsPerGridX - 1) / kRowsPerGridX));
