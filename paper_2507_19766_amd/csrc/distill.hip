@@ -10,7 +10,7 @@
 // the listed probabilities would lose all its digits where the student is sure of them.  What a row is made of after that (K terms)
 // is in 64 bits: a divergence is a small sum of larger terms.
 //
-//   distill_target_kernel   is the target a distribution; what the row's gradient needs of it (rows of one piece: their own workgroups)
+//   distill_target_kernel   is the target a distribution; what the row's gradient needs of it (unless the stream's workgroups do it)
 //   distill_piece_kernel    the stream over the logits: a row's pieces, each a workgroup's registers (a short row a wave's), to (max, S);
 //                           listed logits
 //   distill_row_kernel      one call: the same pieces, which tell each other their sums and write the gradient from the registers
@@ -50,13 +50,18 @@ constexpr int kFinishSmall = 256, kFinishLarge = 1024;
 constexpr int64_t kWaveRow = 512;       // vectors
 constexpr int64_t kManyRows = 2048;
 
+// Where pieces work their row's target out themselves: one to a row, or few enough of them to wait for it all at once; pieces that tell each other
+// their sums need a kernel before them, which clears what they tell them through.  Forward, us, themselves / distill_target_kernel: 1 x 151936
+// bf16 12.2 / 14.8, 256 x 32000 14.4 / 16.5, 256 x 151936 26.3 / 26.3, 1024 x 64000 34.3 / 32.5, 8192 x 32000 (K 128) 127 / 117.
+constexpr int64_t kFewPieces = 1024;
+
 // Listed probabilities may sum to more than 1 by their rounding (log-probs kept in bf16: 2 %); beyond this they are no log-probs.
 constexpr double kMostMass = 1.25;
 
 enum { ROW_ON = 0, ROW_WEIGHTLESS = 1, ROW_EMPTY = 2, ROW_BAD_TOKEN = 3, ROW_BAD_TARGET = 4 };
 
 // What the stream has to know of a row's target: g Q and g q_rest, with g = weight / (D T).  twice: an id is listed twice, which the
-// stream finds (and publishes as a sum that is no number).
+// stream finds (and publishes as a sum that is no number; with own_target in the forward call, as a piece's second word).
 struct RowTarget {
     float mass, rest;
     int32_t state;
@@ -80,7 +85,7 @@ struct DistillArgs {
     float* top_grad;            // [N, K]; the listed logits until the row is finished
     int64_t* counters;          // may be NULL
     RowTarget* target;          // [N]
-    unsigned long long* slots;  // [N * C * 2]: {max, S} of a piece's unlisted logits, {max, S} of its listed ones
+    unsigned long long* slots;  // [N * C * 2]: {max, S} of a piece's unlisted logits, {max, S} of its listed ones (forward: an id twice)
     unsigned long long* pending;    // [N], one call: pieces whose gradient is not written, because a wait expired
     Partial* partial;           // [kFinishGroups]
     uint32_t* flags;            // ticket of the finishing kernel; one call: whether any wait expired
@@ -89,6 +94,7 @@ struct DistillArgs {
     int64_t N, row_stride;
     int32_t V, K, C;
     int32_t tail;
+    int32_t own_target;         // no distill_target_kernel
     float scale;                // log2(e) / T
     double inv_t, inv_D;
 };
@@ -177,7 +183,7 @@ __device__ __forceinline__ RowTarget row_target(const DistillArgs& a, int64_t ro
     return t;
 }
 
-// Rows of several pieces: what all of a row's workgroups have to know.
+// What all of a row's workgroups have to know.
 template <int L>
 __global__ __launch_bounds__(kThreads) void distill_target_kernel(DistillArgs a)
 {
@@ -239,7 +245,7 @@ struct PieceShared {
     int32_t where[kMaxK];       // vector of the thread * 8 + element
     float m[kWaves], top_m[kWaves];
     double S[kWaves], top_S[kWaves];
-    RowTarget target;           // of a row of one piece
+    RowTarget target;           // where the workgroup works it out
     int32_t twice;
 };
 
@@ -264,12 +270,12 @@ __device__ __forceinline__ void load_piece(const typename Tr::elem* rowp, int32_
 }
 
 // A row's target, and its piece c on the way into registers; false: the row does not count (and is not read where its weight is 0).
-// The workgroup of a row of one piece works the target out itself while the row is on its way, and no kernel runs before it.
+// With own_target the workgroups work the target out themselves while the row is on its way, and no kernel runs before them.
 template <class Tr, int VPT, int NT>
 __device__ __forceinline__ bool start_piece(const DistillArgs& a, const typename Tr::elem* rowp, int64_t row, int c, u32x4 (&v)[VPT], RowTarget& target,
                                             PieceShared<NT>& sh)
 {
-    if (a.C > 1) {
+    if (!a.own_target) {
         target = a.target[row];
         if (target.state != ROW_ON) return false;
         load_piece<Tr, VPT, NT>(rowp, a.V, c, v);
@@ -277,7 +283,7 @@ __device__ __forceinline__ bool start_piece(const DistillArgs& a, const typename
     }
     const int tid = threadIdx.x;
     if (a.weights == nullptr || a.weights[row] != 0.0f) load_piece<Tr, VPT, NT>(rowp, a.V, c, v);
-    if (row == 0 && tid < 2) a.flags[tid] = 0u;         // for the kernel that follows
+    if (row == 0 && c == 0 && tid < 2) a.flags[tid] = 0u;       // for the kernel that follows
     if (tid < 64) {
         const RowTarget t = row_target<64>(a, row, tid);
         if (tid == 0) sh.target = t;
@@ -285,7 +291,7 @@ __device__ __forceinline__ bool start_piece(const DistillArgs& a, const typename
     __syncthreads();
     target = sh.target;
     if (target.state == ROW_ON) return true;
-    if (tid == 0) a.target[row] = target;
+    if (tid == 0 && c == 0) a.target[row] = target;
     return false;
 }
 
@@ -373,8 +379,11 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
     __syncthreads();
     PieceSums p = {kFloor, kFloor, 0.0, 0.0};
     if (tid == 0) {
-        if (a.C == 1) a.target[row] = RowTarget{target.mass, target.rest, target.state, sh.twice};
-        else if (sh.twice != 0) a.target[row].twice = 1;
+        if (a.own_target) {
+            if (c == 0) a.target[row] = RowTarget{target.mass, target.rest, target.state, TOP ? sh.twice : 0};
+        } else if (sh.twice != 0) {
+            a.target[row].twice = 1;
+        }
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) p.m = larger(p.m, sh.m[w]);
 #pragma unroll
@@ -414,6 +423,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(1, kMostWave
     if (threadIdx.x == 0) {
         unsigned long long* slot = a.slots + (row * a.C + blockIdx.x) * 2;
         slot[0] = slot_word(p.m, p.S);
+        if (a.own_target) slot[1] = (unsigned long long)sh.twice;
     }
 }
 
@@ -599,7 +609,12 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
             }
         }
         const unsigned long long slot = lane < a.C ? a.slots[(row * a.C + lane) * 2] : 0ull;
-        const int32_t state = target.twice != 0 ? ROW_BAD_TARGET : target.state;
+        bool twice = target.twice != 0;
+        if (a.own_target && a.spin_limit == 0) {
+            for (int c = lane; c < a.C; c += L) twice = twice || a.slots[(row * a.C + c) * 2 + 1] != 0ull;
+            twice = Lanes<L>::any(twice);
+        }
+        const int32_t state = target.state == ROW_ON && twice ? ROW_BAD_TARGET : target.state;
         float grad[2] = {0.0f, 0.0f};
         float kl_out = 0.0f, lse_out = 0.0f, max_out = 0.0f, coef_out = 0.0f;
         if (state == ROW_ON) {
@@ -871,9 +886,10 @@ void launch_top(int64_t N, int64_t V, int64_t row_stride, const int32_t* ids, in
 
 // The forward call, and with dlogits the gradient too.
 template <class Tr>
-int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const DistillArgs& a, hipStream_t st)
+int32_t enqueue(const void* logits, void* dlogits, const Layout& l, DistillArgs a, hipStream_t st)
 {
     using elem = typename Tr::elem;
+    a.own_target = a.C == 1 || (a.spin_limit == 0 && a.N * a.C <= kFewPieces);
     const int L = lanes_of(a.K);
     auto with_lanes = [&](const auto& f) {
         if (L == 16) f(std::integral_constant<int, 16>{});
@@ -881,7 +897,7 @@ int32_t enqueue(const void* logits, void* dlogits, const Layout& l, const Distil
         else f(std::integral_constant<int, 64>{});
     };
     auto groups = [&](int threads) { return (a.N * L + threads - 1) / threads; };
-    if (a.C > 1) with_lanes([&](auto l_) {
+    if (!a.own_target) with_lanes([&](auto l_) {
         hipLaunchKernelGGL((distill_target_kernel<decltype(l_)::value>), dim3((unsigned)groups(kThreads)), dim3(kThreads), 0, st, a);
     });
     if (!launch_stream<Tr>(l, logits, dlogits, a, st)) return ULORL_ERR_HIP;

@@ -316,6 +316,30 @@ def test_rows_that_do_not_count(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n", [60, 900])
+def test_ids_listed_twice_in_any_piece(n, dtype):
+    V, K = 50003, 70
+    z, ids, logp, w = problem(n, V, K, dtype, 4)
+    w = w.abs() + 0.1
+    bad = list(range(0, n, 7))
+    for i, r in enumerate(bad):
+        ids[r, (5 * i) % 60] = ids[r, 60 + i % 10] = (i * 4001) % V         # in every piece of a row
+    assert (ids[bad].long().sort(1).values.diff(dim=1) == 0).any(1).all()
+    w[n - 1] = 0.0
+    good = torch.ones(n, dtype=torch.bool, device=DEV)
+    good[bad] = good[n - 1] = False
+    ref, tol = reference(z[good], ids[good], logp[good], w[good], ulorl.DistillParams(denominator=n))
+    def look(r, d):
+        assert r.counters.tolist() == [int(good.sum()), 1 if n - 1 not in bad else 0, 0, 16]
+        assert (r.kl[~good] == 0).all() and (d[~good] == 0).all() and (r.top_grad[~good] == 0).all()
+        compare(dict(kl=r.kl[good], lse=r.lse[good], loss=r.loss, dlogits=d[good]), ref, tol, dtype)
+    look(*ulorl.distill_fwd_bwd(z, ids, logp, w))
+    r = ulorl.distill_fwd(z, ids, logp, w)
+    look(r, ulorl.distill_bwd(z, ids, r))
+    look(*ulorl.distill_fwd_bwd(z, ids, logp, w, launch=ulorl.Launch(per_row=True)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("n,V", [(5, 4096), (70, 151936), (300, 32003)])
 def test_in_place_and_strided(n, V, dtype):
     """Over the logits the same bits; what lies between the rows is left alone; the same call twice gives the same bits."""
