@@ -313,8 +313,8 @@ int32_t ulorl_token_loss_fwd_bwd_static(
  * not-a-number or +infinity, or nothing but masked logits, gets not-a-number everywhere and ids of -1.
  * Sums are exact to about 1e-7 for logits up to 1e8 temperature; beyond that a row may be reported as not finite.
  *   workspace     ulorl_token_topk_workspace_bytes(N, V) bytes, 256-byte aligned, or NULL.  With one, few rows
- *                 are read by several workgroups each; without, every row by one.  The same ids either way;
- *                 sums differ by their order.  Its contents need not be preserved between calls.
+ *                 are read by several workgroups each; without, every row by one.  The same ids either way, and
+ *                 however many rows there are; sums differ by their order.  Its contents need not be preserved between calls.
  */
 size_t ulorl_token_topk_workspace_bytes(int64_t N, int64_t V);
 
@@ -350,13 +350,15 @@ int32_t ulorl_token_topk(
  *                 RENORM: all of probability 0), status word
  * Rows that do not count (kl, gradient and lse are 0): weight 0; nothing listed; and with a status bit an id >= V
  * (ULORL_STATUS_BAD_TOKEN), an id twice, a log-prob that is not-a-number or +infinity, probabilities that sum to more
- * than 1.25 (BUCKET, DROP: the values are no log-probs), or a weight that is not finite (ULORL_STATUS_BAD_TARGET).  A row that has not-a-number or +infinity among its logits, nothing unmasked, or a masked
- * token to which the teacher gives probability raises ULORL_STATUS_NONFINITE: kl and gradient 0, lse as it comes.
+ * than 1.25 (BUCKET, DROP: the values are no log-probs), or a weight that is not finite (ULORL_STATUS_BAD_TARGET).
+ * A row that has not-a-number or +infinity among its logits, nothing unmasked, or a masked token to which the teacher
+ * gives probability raises ULORL_STATUS_NONFINITE: kl and gradient 0, lse as it comes.
  *   workspace     >= ulorl_distill_workspace_bytes(N, V, dt) bytes, 256-byte aligned; need not be preserved.
  *
  * ulorl_distill_fwd      loss and per-row outputs; one read of the logits
  * ulorl_distill_bwd      dlogits from them; type and stride of logits, MAY BE THE SAME BUFFER.  grad_out: HOST scalar;
- *                        grad_scale: DEVICE scalar that multiplies it, or NULL
+ *                        grad_scale: DEVICE scalar that multiplies it, or NULL.  One that is not finite makes the
+ *                        gradient of the rows that count not finite
  * ulorl_distill_fwd_bwd  both, with one read and one write of HBM per row: as in ulorl_token_loss_fwd_bwd a row is shared
  *                        by workgroups that exchange their sums, with a bounded wait (what one that waited in vain left
  *                        undone is written before the call's last kernel ends).  launch: HOST, may be NULL:

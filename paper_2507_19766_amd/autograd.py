@@ -99,6 +99,8 @@ class _FusedDistill(torch.autograd.Function):
             raise RuntimeError("distill_loss(fused=True) computed the gradient of an upstream 1 in its forward pass; "
                                "got an upstream gradient of %r: scale through DistillParams.denominator or use fused=False" % g)
         d = ctx.dlogits
+        if d is None:
+            raise RuntimeError("distill_loss(fused=True) has given its gradient away in an earlier backward pass; use fused=False")
         ctx.dlogits = None
         return (d,) + (None,) * 7
 

@@ -432,10 +432,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(1, kMostWave
 // (|m scale| and |log2 c| are tens) would be ten units of the result, c 2^((z - m) scale).
 struct RestGradient {
     float c, m, shift, scale;
-    bool none;                  // zeros: no coefficient, or one that is no number
+    bool none;                  // zeros: no coefficient
     __device__ __forceinline__ RestGradient(float coef, float max, float scale_) : c(coef), m(max), scale(scale_)
     {
-        none = c == 0.0f || !finite(c);
+        none = c == 0.0f;
         shift = none ? 0.0f : fmaf(-m, scale, log2f(fabsf(c)));
     }
     template <class Tr>
@@ -469,11 +469,15 @@ __device__ __forceinline__ void store_vector(typename Tr::elem* outp, int32_t V,
     }
 }
 
-// A listed token's gradient; what is no number leaves 0, as in RestGradient.
+// A row's gradient (a coefficient of it) under an upstream one: of rows that do not count 0, whatever the upstream is; of others what that
+// makes of it, infinities and not-a-number included.
+__device__ __forceinline__ float under(float g, float upstream) { return g == 0.0f ? 0.0f : g * upstream; }
+
+// A listed token's gradient.
 template <class Tr>
 __device__ __forceinline__ void store_top(typename Tr::elem* outp, int32_t V, int32_t id, float g)
 {
-    if (id >= 0 && id < V) Tr::store1(outp + id, finite(g) ? g : 0.0f);
+    if (id >= 0 && id < V) Tr::store1(outp + id, g);
 }
 
 // One call: the pieces of a row keep their logits in registers, tell each other their sums and write the gradient of their
@@ -538,7 +542,8 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(const typename Tr::elem
         const double top = wave_sum_f64((double)fast_exp2((tm - M) * a.scale) * tS);            // relative to M
         const double R = (double)fast_exp2((rest_max - M) * a.scale) * rest;
         if (tid == 0) {
-            bc_coef = rest != 0.0 ? (float)(((double)target.mass * (R / (R + top)) - (double)target.rest) / rest) * a.grad_out : 0.0f;
+            const float coef = rest != 0.0 ? (float)(((double)target.mass * (R / (R + top)) - (double)target.rest) / rest) : 0.0f;
+            bc_coef = finite(coef) ? under(coef, a.grad_out) : 0.0f;        // no number: a row that does not count
             bc_max = rest_max;
             bc_expired = expired;
             if (expired) {
@@ -696,7 +701,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
         for (int h = 0; h < 2; ++h) {
             if (lane + L * h < a.K) top[lane + L * h] = grad[h];
             // one call: the unlisted tokens' gradients are there already
-            if (a.spin_limit > 0 && state == ROW_ON) store_top<Tr>(dlogits + row * a.row_stride, a.V, id[h], grad[h] * a.grad_out);
+            if (a.spin_limit > 0 && state == ROW_ON) store_top<Tr>(dlogits + row * a.row_stride, a.V, id[h], under(grad[h], a.grad_out));
         }
         if (lane == 0) {
             a.kl[row] = kl_out;
@@ -710,7 +715,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
         const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
         for (int64_t row = (int64_t)blockIdx.x * ROWS + (int)threadIdx.x / L; row < a.N; row += (int64_t)gridDim.x * ROWS) {
             for (unsigned long long todo = a.pending[row]; todo != 0ull; todo &= todo - 1ull) {
-                const RestGradient rest(a.rest_coef[row] * a.grad_out, a.rest_max[row], a.scale);
+                const RestGradient rest(under(a.rest_coef[row], a.grad_out), a.rest_max[row], a.scale);
                 const int begin = (__ffsll((long long)todo) - 1) * piece_vectors;
                 for (int i = begin + lane; i < min(all, begin + piece_vectors); i += L)
                     store_vector<Tr>(dlogits + row * a.row_stride, a.V, i,
@@ -719,7 +724,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
             if (a.pending[row] == 0ull) continue;
             __threadfence();                        // the listed tokens' again, over them
             for (int j = lane; j < a.K; j += L)
-                store_top<Tr>(dlogits + row * a.row_stride, a.V, a.ids[row * a.K + j], a.top_grad[row * a.K + j] * a.grad_out);
+                store_top<Tr>(dlogits + row * a.row_stride, a.V, a.ids[row * a.K + j], under(a.top_grad[row * a.K + j], a.grad_out));
         }
     }
     // a row's first lane has what it contributed
@@ -775,7 +780,7 @@ __global__ __launch_bounds__(kThreads) void distill_dense_kernel(const typename 
 {
     const int64_t row = (int64_t)blockIdx.z * kRowsPerGridY + blockIdx.y;
     if (row >= N) return;
-    const RestGradient grad(rest_coef[row] * (grad_scale ? *grad_scale * grad_out : grad_out), rest_max[row], scale);
+    const RestGradient grad(under(rest_coef[row], grad_scale ? *grad_scale * grad_out : grad_out), rest_max[row], scale);
     const int i = (int)blockIdx.x * kThreads + (int)threadIdx.x;
     u32x4 o = {0u, 0u, 0u, 0u};
     if (!grad.none) o = grad.template of<Tr>(load_vector<Tr>(logits + row * row_stride, V, i));
@@ -788,7 +793,7 @@ __global__ __launch_bounds__(kThreads) void distill_top_kernel(const int32_t* id
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (i >= N * K) return;
-    store_top<Tr>(dlogits + (i / K) * row_stride, V, ids[i], top_grad[i] * (grad_scale ? *grad_scale * grad_out : grad_out));
+    store_top<Tr>(dlogits + (i / K) * row_stride, V, ids[i], under(top_grad[i], grad_scale ? *grad_scale * grad_out : grad_out));
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -430,6 +430,38 @@ def test_autograd_scales_and_repeats():
     assert not ulorl.autograd.distill_loss(z, ids, logp, w, p).requires_grad
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("up", [math.nan, math.inf, -math.inf])
+def test_an_upstream_gradient_that_is_not_finite(up, dtype):
+    """Not hidden: rows that count are not finite (a bucket's tokens have a gradient each), the others' gradient stays 0."""
+    for n, V in [(40, 3000), (30, 40003), (2100, 600)]:
+        z, ids, logp, w = problem(n, V, 10, dtype, 6)
+        w = w.abs() + 0.1
+        w[3], w[n - 1] = 0.0, 0.0
+        z[7, 5] = math.nan
+        z[8, 11] = -math.inf
+        ids[9, 2] = V
+        off = torch.zeros(n, dtype=torch.bool, device=DEV)
+        off[[3, n - 1, 7, 9]] = True
+        r = ulorl.distill_fwd(z, ids, logp, w)
+        scale = torch.tensor(up, device=DEV)
+        leaf = z.detach().requires_grad_(True)
+        (ulorl.autograd.distill_loss(leaf, ids, logp, w) * up).backward()
+        for d in (ulorl.distill_bwd(z, ids, r, grad_scale=scale), ulorl.distill_bwd(z, ids, r, grad_out=up),
+                  ulorl.distill_fwd_bwd(z, ids, logp, w, grad_out=up)[1],
+                  ulorl.distill_fwd_bwd(z, ids, logp, w, grad_out=up, launch=ulorl.Launch(sync_spins=1))[1], leaf.grad):
+            assert (d[off] == 0).all()
+            assert (~d[~off].isfinite()).any(1).all()
+
+
+def test_a_fused_gradient_is_given_once():
+    z, ids, logp, w = problem(20, 3000, 10, F, 6)
+    loss = ulorl.autograd.distill_loss(z.clone().requires_grad_(True), ids, logp, w, fused=True)
+    loss.backward(retain_graph=True)
+    with pytest.raises(RuntimeError, match="earlier backward"):
+        loss.backward()
+
+
 def test_beside_the_token_loss():
     """The two objectives on the same logits: the gradient of their sum is the sum of their gradients."""
     z, ids, logp, w = problem(64, 5000, 10, F, 9)
