@@ -303,8 +303,8 @@ int32_t ulorl_token_loss_fwd_bwd_static(
  * shows of its alternatives, and what is recorded of a teacher for ulorl_distill_*.
  * With x = z / temperature and p = softmax(x):
  *   lse       [N]      ln sum_j e^x_j                     entropy  [N]  - sum_j p_j ln p_j, nats
- *   logp      [N]      x[token_ids] - lse; not-a-number for an id outside [0, V).  token_ids may be NULL (logp is
- *                      not written then and may be NULL)
+ *   logp      [N]      x[token_ids] - lse, -infinity of a masked token; not-a-number for an id outside [0, V).
+ *                      token_ids may be NULL (logp is not written then and may be NULL)
  *   top_ids   [N, K]   int32, the K largest logits in falling order; of equal logits (+0 and -0 are) the lower id first
  *   top_logp  [N, K]   their x - lse
  * logits, N, V and row_stride as in ulorl_token_loss_fwd, N < 2^31; 1 <= K <= 128; temperature in [1e-3, 1e3].

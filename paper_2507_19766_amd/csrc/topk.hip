@@ -513,7 +513,8 @@ __device__ __forceinline__ Token token_of(const TopkArgs& a, const typename Tr::
 {
     const int32_t y = a.token_ids ? a.token_ids[row] : -1;
     const bool has = y >= 0 && y < a.V;
-    return Token{has, has ? Tr::load1(rowp + y) : 0.0f};
+    const float z = has ? Tr::load1(rowp + y) : 0.0f;
+    return Token{has, z <= kFloor ? -INFINITY : z};         // masked: of probability 0
 }
 
 // A row's results from its statistics and its groups' maxima in sh.gmax.  All threads call it after a barrier.

@@ -183,6 +183,20 @@ def test_masked_logits(mask, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("mask", [-math.inf, "lowest", -1e30])
+def test_given_tokens_that_are_masked(mask, dtype):
+    value = torch.finfo(dtype).min if mask == "lowest" else mask
+    for n, V in [(1, 151936), (6, 32003), (1100, 2000)]:
+        z = rows(n, V, dtype, 4)
+        y = tokens(n, V, 2)
+        for T in (1.0, 0.01, 100.0):
+            masked = torch.arange(n, device=DEV) % 2 == 0
+            z[masked, y[masked].long()] = value
+            r = ulorl.token_topk(z, 3, y, temperature=T)
+            assert (r.logp[masked] == -math.inf).all() and r.logp[~masked].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_peaked_rows(dtype):
     """One logit far above all others: the log-prob of that token is the small sum of the others."""
     z = rows(8, 151936, dtype, 11)
