@@ -131,11 +131,12 @@ __device__ __forceinline__ double exp64(double x)
     p = fma(p, f, 1.0);
     return ldexp(p, (int)n);
 }
-// One Newton step from the 32-bit logarithm: its error squared.  For x within the range of 32 bits.
+// A step of second order from the 32-bit logarithm: its error (1e-6 where the logarithm is 12) cubed.  For x within the range of 32 bits.
 __device__ __forceinline__ double log64(double x)
 {
     const double l = (double)__builtin_amdgcn_logf((float)x) * 0.69314718055994530942;
-    return l + fma(x, exp64(-l), -1.0);
+    const double r = fma(x, exp64(-l), -1.0);       // ln(1 + r) is missing
+    return l + fma(-0.5 * r, r, r);
 }
 
 }  // namespace ulorl_detail

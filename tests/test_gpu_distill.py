@@ -148,6 +148,16 @@ def test_tails_and_temperatures(tail, T, dtype):
         check(z, ids, logp, None, p, ("one",))
 
 
+@pytest.mark.parametrize("tail", TAILS)
+@pytest.mark.parametrize("T", [5.0, 30.0, 1000.0])
+def test_a_divergence_of_flat_distributions(tail, T):
+    """kl of 1e-11 and less beside logarithms of 12: what is in 64 bits is as good as 64 bits."""
+    p = ulorl.DistillParams(temperature=T, tail=tail)
+    for n, V, dtype in [(2, 151936, F), (2100, 1000, F), (2, 151936, BF), (300, 20000, BF)]:
+        z, ids, logp, w = problem(n, V, 20, dtype, 3, T, tail=tail)
+        check(z, ids, logp, w, p, ("one", "two"))
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 255, 2047, 2048, 2049, 8192, 15359, 15360, 15361, 16385, 30719, 30720, 30721, 61439, 61441, 100003])
 def test_lengths_of_rows(V, dtype):
