@@ -197,6 +197,13 @@ def test_given_tokens_that_are_masked(mask, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("T", [0.001, 0.05, 0.2, 5.0, 30.0, 1000.0])
+def test_temperatures(T, dtype):
+    for n, V in [(3, 32003), (1100, 3000), (2, 151936), (300, 20000)]:
+        check(rows(n, V, dtype, 1), 20, T, tokens(n, V), lanes=64)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_peaked_rows(dtype):
     """One logit far above all others: the log-prob of that token is the small sum of the others."""
     z = rows(8, 151936, dtype, 11)
