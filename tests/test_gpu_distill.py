@@ -161,6 +161,15 @@ def test_peaked_and_flat_distributions(tail, T):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("mean,std", [(1e4, 3.0), (-1e4, 3.0), (1e6, 3.0), (-3e7, 100.0), (0.0, 1e5), (50.0, 0.0)])
+def test_logits_of_any_size(mean, std, dtype):
+    for n, V in [(3, 32003), (2100, 1000), (300, 20000)]:
+        z, ids, logp, w = problem(n, V, 20, dtype, 3)
+        z.copy_((z.float() / 3 * std + mean).to(dtype))
+        check(z, ids, logp, w, ulorl.DistillParams(), ("one", "two"))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 255, 2047, 2048, 2049, 8192, 15359, 15360, 15361, 16385, 30719, 30720, 30721, 61439, 61441, 100003])
 def test_lengths_of_rows(V, dtype):
     for n, K, tail in [(1, 1, ulorl.TAIL_BUCKET), (3, 64, ulorl.TAIL_BUCKET), (2, 128, ulorl.TAIL_DROP), (4, 5, ulorl.TAIL_RENORM)]:

@@ -204,6 +204,15 @@ def test_temperatures(T, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("mean,std", [(1e4, 3.0), (-1e4, 3.0), (1e6, 3.0), (-3e7, 100.0), (0.0, 1e5), (50.0, 0.0)])
+def test_logits_of_any_size(mean, std, dtype):
+    for n, V in [(3, 32003), (2100, 1000), (300, 20000)]:
+        z = rows(n, V, dtype, 1, std=1.0)
+        z.copy_((z.float() * std + mean).to(dtype))
+        check(z, 20, 1.0, tokens(n, V), lanes=64)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_peaked_rows(dtype):
     """One logit far above all others: the log-prob of that token is the small sum of the others."""
     z = rows(8, 151936, dtype, 11)
