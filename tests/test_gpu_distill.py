@@ -361,6 +361,24 @@ def test_ids_listed_twice_in_any_piece(n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("between", [math.nan, math.inf, 1e4])
+def test_what_lies_between_rows_is_left_alone(between, dtype):
+    vec = 8 if dtype == BF else 4
+    for n, V in [(2100, 1001), (2100, 130), (700, 5003), (3, 32003), (70, 151931), (5, 3)]:
+        base = torch.full((n + 1, V + (-V % vec) + vec), between, dtype=dtype, device=DEV)
+        z = base[:n, :V]
+        given, ids, logp, w = problem(n, V, 20, dtype, 3)
+        z.copy_(given)
+        check(z, ids, logp, w, ulorl.DistillParams(), ("one", "two"))
+        before = base.clone()
+        ulorl.distill_fwd_bwd(z, ids, logp, w, inplace=True)
+        outside = torch.ones_like(base, dtype=torch.bool)
+        outside[:n, :V] = False
+        assert torch.equal(before[outside].view(torch.int16 if dtype == BF else torch.int32),
+                           base[outside].view(torch.int16 if dtype == BF else torch.int32))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("n,V", [(5, 4096), (70, 151936), (300, 32003)])
 def test_in_place_and_strided(n, V, dtype):
     """Over the logits the same bits; what lies between the rows is left alone; the same call twice gives the same bits."""

@@ -213,6 +213,17 @@ def test_logits_of_any_size(mean, std, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("between", [math.nan, math.inf, 1e4])
+def test_what_lies_between_rows_is_not_looked_at(between, dtype):
+    vec = 8 if dtype == BF else 4
+    for n, V in [(1100, 1001), (1100, 4099), (3, 32003), (1, 151935), (70, 151931), (5, 3)]:
+        base = torch.full((n + 1, V + (-V % vec) + vec), between, dtype=dtype, device=DEV)
+        z = base[:n, :V]
+        z.copy_(rows(n, V, dtype, 1))
+        check(z, 20, 1.0, tokens(n, V), lanes=64)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_peaked_rows(dtype):
     """One logit far above all others: the log-prob of that token is the small sum of the others."""
     z = rows(8, 151936, dtype, 11)
