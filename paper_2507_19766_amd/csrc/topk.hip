@@ -45,15 +45,15 @@ constexpr int groups_per_lane(int nt) { return nt <= 256 ? 10 : 2560 / nt; }
 constexpr int max_groups(int nt) { return nt * groups_per_lane(nt); }     // group maxima of a row: 10 KB of LDS with 256 threads
 constexpr int kMaxGroups = max_groups(kTopkThreads);                  // and of a split row's, with 512
 constexpr uint32_t kOverflow = 0xffffffffu;
-// Where rows are split: few of them, each long.  us, split / one workgroup a row: 1 row of 151936 bf16 12 / 16, fp32 12 / 25; 128 rows 20 / 23 and
-// 24 / 29; 256 rows 26 / 24 and 36 / 32; 1 row of 32000 bf16 11.5 / 9.1.
+// Where rows are split: few of them, each long.  us, split / one workgroup a row, K 8: 1 row of 151936 bf16 11 / 16, fp32 11 / 25; 100 rows 15.2 / 20.8
+// and 18.3 / 27.3; 200 rows 20.1 / 21.6 and 28.0 / 29.0; 256 rows 22.9 / 22.1 and 33.5 / 30.3; 1 row of 32000 bf16 11.5 / 9.1.
+constexpr int kMaxPieces = 64;
+constexpr int64_t kSplitRows = 200;
+constexpr int64_t kSplitBatches = 8;          // of 16 KB
+constexpr int64_t kFewWorkgroups = 1024;
 // Of the workgroup that finishes a split row, whose chain of steps is what such a call waits for.  us with 256 / 512 / 1024, K 20 (K 128):
 // 1 row of 151936 bf16 11.5 / 10.9 / 13.2 (17 / 14 / 16), 64 rows 15.1 / 15.1 / 17.0 (28 / 20.5 / 20.2).
 constexpr int kMergeThreads = 512;
-constexpr int kMaxPieces = 64;
-constexpr int64_t kSplitRows = 160;
-constexpr int64_t kSplitBatches = 8;          // of 16 KB
-constexpr int64_t kFewWorkgroups = 1024;
 
 // Where one wave does a row: short rows, enough of them to fill the chip.  No barriers, and what a row costs besides its stream (joining
 // the lanes, the search) is done once instead of by four waves.  us with K 10, wave / workgroup of four: 20000 x 2048 fp32 37 / 84, 20000 x

@@ -87,6 +87,13 @@ def test_long_rows(n, V, dtype):
         check(rows(n, V, dtype, k), k, 1.0, tokens(n, V))
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n", [64, 160, 199, 200, 201])
+def test_numbers_of_long_rows(n, dtype):
+    for k in (1, 40, 128):
+        check(rows(n, 70001, dtype, n + k), k, 1.0, tokens(n, 70001))
+
+
 @pytest.mark.parametrize("n", [1, 2, 63, 255, 256, 257, 1023, 2049])
 def test_numbers_of_rows(n):
     check(rows(n, 32003, BF, n), 33, 1.0, tokens(n, 32003))
