@@ -24,6 +24,7 @@
 
 #include <type_traits>
 
+#include "kth_key.hpp"
 #include "logits_stream.hpp"
 #include "row_sums.hpp"
 #include "ulorl.h"
@@ -214,7 +215,7 @@ __device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared<NT
     return r;
 }
 
-// Number of threads' items that hold, over the workgroup (uniform).  turn alternates, so that one barrier a call is enough.
+// Number of threads' items that hold, over the workgroup (uniform).  turn is one more with every call, so that one barrier a call is enough.
 template <int NT>
 __device__ __forceinline__ uint32_t block_count(uint32_t mine, int turn, Shared<NT>& sh)
 {
@@ -227,26 +228,16 @@ __device__ __forceinline__ uint32_t block_count(uint32_t mine, int turn, Shared<
     return n;
 }
 
-// A key that exactly K of the ranked keys reach, all of them where there are fewer; ids are below n.  each(f) calls f(key) for every
-// key of this thread.  Of a key's lower half only the bits that ids differ in are looked for.
+// kth_key over the keys of all threads: each(f) calls f(key) for every key of this thread.
 template <int NT, class Each>
 __device__ uint64_t kth_ranked(const Each& each, uint32_t K, uint32_t n, Shared<NT>& sh)
 {
-    const int id_bits = 32 - __builtin_clz(n);
-    uint64_t t = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        if (bit < 32 && bit >= id_bits) {
-            t |= 1ull << bit;
-            continue;
-        }
-        const uint64_t c = t | (1ull << bit);
+    const uint64_t t = kth_key(K, n, [&](uint64_t c, int turn) {
         uint32_t mine = 0;
         each([&](uint64_t key) { mine += key >= c ? 1u : 0u; });
-        const uint32_t reach = block_count(mine, bit, sh);
-        if (reach >= K) t = c;
-        if (reach == K) break;
-    }
-    __syncthreads();
+        return block_count(mine, turn, sh);
+    });
+    __syncthreads();            // the next search starts at turn 0 again
     return t;
 }
 
