@@ -311,7 +311,9 @@ int32_t ulorl_token_loss_fwd_bwd_static(
  * A logit at or below -9e29, -infinity included, is MASKED: it has probability 0 and is no alternative; where
  * fewer than K tokens are left (V < K too) the last ids are -1 and their log-probs -infinity.  A row that holds
  * not-a-number or +infinity, or nothing but masked logits, gets not-a-number everywhere and ids of -1.
- * Sums are exact to about 1e-7 for logits up to 1e8 temperature; beyond that a row may be reported as not finite.
+ * Results are exact to about 1e-7 of themselves whatever V, at worst (rows of few values, whose roundings are alike, most of them
+ * tens of nats below the largest) lse to 3e-7 and the entropy to 1.2e-6, for logits up to 1e8 temperature; beyond that a row
+ * may be reported as not finite.
  *   workspace     ulorl_token_topk_workspace_bytes(N, V) bytes, 256-byte aligned, or NULL.  With one, few rows
  *                 are read by several workgroups each; without, every row by one.  The same ids either way, and
  *                 however many rows there are; sums differ by their order.  Its contents need not be preserved between calls.

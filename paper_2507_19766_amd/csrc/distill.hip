@@ -349,7 +349,7 @@ __device__ __forceinline__ PieceSums piece_sums(const DistillArgs& a, const type
             if (k == k_j) take_out<Tr>(v[k], e);
     }
 
-    Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
+    Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f, 0.0f};
     absorb_rest<Tr, VPT, 0>(v, a.scale, acc);
     const float wm = wave_max(acc.m);
     // z scale - mL differs from (z - m) scale by the rounding of mL: taken out here (nothing to take out of an empty lane)

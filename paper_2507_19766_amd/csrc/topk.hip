@@ -194,7 +194,7 @@ __device__ __forceinline__ Row merge_lanes(const Lane& a, float scale, Shared<NT
     const float d = fmaf(a.m - wm, scale, -delta);
     const float s = a.S == 0.0f ? 0.0f : fast_exp2(d);       // nothing but masked logits: delta is anything there
     const double S = (double)s * ((double)a.S + (double)a.Sc);
-    const double T = (double)s * ((double)a.T + (double)d * (double)a.S);
+    const double T = (double)s * (((double)a.T + (double)a.Tc) + (double)d * ((double)a.S + (double)a.Sc));
     const double wS = wave_sum_f64(S), wT = wave_sum_f64(T);
     if ((threadIdx.x & 63) == 0) {
         sh.m[wave] = wm;
@@ -466,7 +466,7 @@ __device__ __forceinline__ Lane stream_vectors(const TopkArgs& a, const typename
             }
         }
     };
-    Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f};
+    Lane acc = {kFloor, kFloor * a.scale, 0.0f, 0.0f, 0.0f, 0.0f};
     auto take = [&](const u32x4* v, int first, auto whole) {
         const u32x4 four[4] = {v[0], v[1], v[2], v[3]};
         float vm[4];
