@@ -109,8 +109,8 @@ def distill_loss(logits: torch.Tensor, teacher_ids, teacher_logp, weights=None, 
                  fused: bool = False, in_place: bool = False, launch: Optional[Launch] = None,
                  results: Optional[list] = None) -> torch.Tensor:
     """The weighted mean divergence of each row from its teacher's listed tokens as a differentiable 0-dim tensor (gradient to
-    ``logits`` only).  ``fused`` and ``in_place`` as in ``token_loss``; ``results``: a list that receives the call's
-    ``DistillResult``."""
+    ``logits`` only; a ``teacher_logp`` or ``weights`` that requires one makes the loss a node of the graph and gets none).
+    ``fused`` and ``in_place`` as in ``token_loss``; ``results``: a list that receives the call's ``DistillResult``."""
     if fused:
         return _FusedDistill.apply(logits, teacher_ids, teacher_logp, weights, params, in_place, launch, results)
     if in_place:

@@ -471,7 +471,7 @@ std::pair<Tensor, Tensor> lmhead_bwd(const Tensor& h, const Tensor& w, const Opt
 
 // ------------------------------------------------------------------------------------------ autograd
 // The upstream gradient is a 0-dim device tensor; it is multiplied into the saved coefficients on the device (the fp32
-// product that the kernels form with a host scalar), so that nothing waits for the GPU.  The objective's float tensors are
+// product that the kernels form with a host scalar), so that nothing waits for the GPU.  The objective's (the target's) float tensors are
 // arguments of the nodes, so that one of them that requires a gradient makes the loss require one (it gets none).
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
@@ -493,7 +493,7 @@ struct TokenLossNode : torch::autograd::Function<TokenLossNode> {
 
 // The upstream gradient goes to the kernels as the device scalar that it is.
 struct DistillNode : torch::autograd::Function<DistillNode> {
-    static Tensor forward(AutogradContext* ctx, const Tensor& logits, const Teacher* t, DistillFields* f)
+    static Tensor forward(AutogradContext* ctx, const Tensor& logits, const Tensor&, const OptTensor&, const Teacher* t, DistillFields* f)
     {
         distill_fwd(logits, *t, std::nullopt, std::nullopt, *f);
         ctx->save_for_backward({logits, t->ids, (*f)[DIS_REST_MAX], (*f)[DIS_REST_COEF], (*f)[DIS_TOP_GRAD]});
@@ -504,7 +504,7 @@ struct DistillNode : torch::autograd::Function<DistillNode> {
     {
         const variable_list s = ctx->get_saved_variables();
         return {distill_bwd(s[0], s[1], s[2], s[3], s[4], ctx->saved_data["temperature"].toDouble(), 1.0, grad[0], std::nullopt, false), Tensor(),
-                Tensor()};
+                Tensor(), Tensor(), Tensor()};
     }
 };
 
@@ -635,7 +635,7 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
     m.def("autograd_distill", [](const Tensor& z, const Tensor& ids, const Tensor& logp, const OptTensor& weights, uintptr_t params, bool want_fields) {
         const Teacher t{ids, logp, weights, reinterpret_cast<const ulorl_distill_params*>(params)};
         DistillFields f;
-        const Tensor loss = unlocked([&] { return DistillNode::apply(z, &t, &f); });
+        const Tensor loss = unlocked([&] { return DistillNode::apply(z, t.logp, t.weights, &t, &f); });
         return py::make_tuple(loss, want_fields ? list_of(f) : py::list());
     });
     m.def("lmhead_fwd", [](const Tensor& h, const Tensor& w, OptTensor y, OptTensor cu, OptTensor adv, OptTensor old, OptTensor ids,
