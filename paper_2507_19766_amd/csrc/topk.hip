@@ -57,10 +57,12 @@ constexpr int64_t kFewWorkgroups = 1024;
 constexpr int kMergeThreads = 512;
 
 // Where one wave does a row: short rows, enough of them to fill the chip.  No barriers, and what a row costs besides its stream (joining
-// the lanes, the search) is done once instead of by four waves.  us with K 10, wave / workgroup of four: 20000 x 2048 fp32 37 / 84, 20000 x
-// 8192 bf16 64 / 106, 20000 x 16384 bf16 115 / 141, 4096 x 4096 fp32 16.5 / 21.5, 1024 x 4096 fp32 8.7 / 9.2; and where it is not taken,
-// 256 x 4096 fp32 8.0 / 6.4, 1024 x 16384 bf16 14.6 / 12.4, 20000 x 32000 bf16 (K 33) 226 / 226.  Rows as many as vectors in one, and
-// 1024, is where both are alike.
+// the lanes, the search) is done once instead of by four waves.  us, wave / workgroup of four, K 10, 64 and 128: 20000 x 2048 fp32
+// 38 / 93, 51 / 102 and 86 / 148, 20000 x 8192 bf16 64 / 102, 87 / 122 and 135 / 173, 20000 x 16384 bf16 112 / 136, 141 / 157 and 211 / 218,
+// 4096 x 4096 fp32 14.8 / 22.5, 19 / 26 and 33 / 41; and where it is not taken, K 10, 256 x 4096 fp32 8.0 / 6.4, 1024 x 16384 bf16 14.6 / 12.4,
+// 20000 x 32000 bf16 (K 33) 226 / 226.  Rows as many as vectors in one, and 1024, is where both are alike with K 64 (1024 x 4096 fp32 10.3 /
+// 10.1, 2048 x 16384 bf16 23.6 / 22.9); there a wave is up to 16 % faster with K 10 (7.3 / 8.7, 17.9 / 20.5) and up to 10 % slower with K 128
+// (19.4 / 17.7, 36.7 / 33.4), whose ranks are a larger part.
 constexpr int kWaveRow = 2048;        // vectors
 constexpr int64_t kManyRows = 1024;
 static_assert(kWaveRow <= (max_groups(64) << 2), "a wave's row has groups of four vectors at most");
@@ -538,11 +540,13 @@ constexpr int64_t kRowsPerGridX = 1 << 20;
 __device__ __forceinline__ int64_t row_of_grid() { return (int64_t)blockIdx.y * kRowsPerGridX + blockIdx.x; }
 
 // One workgroup per row.  At 151936 bf16 logits and K 64 it reads 6.4 TB/s (the statistics alone: 7.0): its vector ALUs are
-// 85 % busy, the search adds instructions (K 33: 7 %, K 128: 29 %) and 6 us in which a workgroup loads little; four workgroups share a
+// 89 % busy, the search adds instructions (to those of ulorl_token_loss_fwd's statistics, K 1: 7 %, K 33: 11 %, K 128: 33 %) and 6 us in
+// which a workgroup loads little; four workgroups share a
 // compute unit (five, with registers in scratch memory for it, 20 % slower; 12 loads in flight instead of 8, three workgroups, 2 %).
-// Short rows take 70 registers for seven (eight: scratch, 8000 x 32000 124 us instead of 104).
+// Short rows take 72 registers for seven (eight: scratch, 8000 x 32000 124 us instead of 104), in fp32 64 for eight (seven: 2000 x 64000
+// 87 us instead of 83, a second round).
 template <class Tr, int LG, int U, int NT>
-__global__ __launch_bounds__(NT, U == 4 && NT == 256 ? 7 : 1) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
+__global__ __launch_bounds__(NT, U == 4 && NT == 256 ? (Tr::kPerVec == 4 ? 8 : 7) : 1) void topk_row_kernel(const typename Tr::elem* __restrict__ logits, TopkArgs a)
 {
     __shared__ Shared<NT> sh;
     const int64_t row = row_of_grid();
