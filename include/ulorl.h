@@ -363,7 +363,8 @@ int32_t ulorl_token_topk(
  *                        gradient of the rows that count not finite
  * ulorl_distill_fwd_bwd  both, with one read and one write of HBM per row: as in ulorl_token_loss_fwd_bwd a row is shared
  *                        by workgroups that exchange their sums, with a bounded wait (what one that waited in vain left
- *                        undone is written before the call's last kernel ends).  launch: HOST, may be NULL:
+ *                        undone is written before the call's last kernel ends; it costs time and is not reported: these calls do
+ *                        not raise ULORL_STATUS_SYNC).  launch: HOST, may be NULL:
  *                        ULORL_LAUNCH_PER_ROW takes the two calls' kernels instead (as rows beyond 64 pieces do: their
  *                        gradient is that of the two calls bit for bit, otherwise to rounding), sync_spins bounds the
  *                        wait; the rest is not looked at.
