@@ -712,7 +712,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const typename Tr::e
     }
     if (a.spin_limit > 0 && a.flags[1] != 0u) {     // pieces whose workgroup waited in vain: their logits are whole, in place too
         __threadfence();                            // the rows' results are these lanes' own
-        const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
+        const int all = vectors_of<Tr>(a.V);
         for (int64_t row = (int64_t)blockIdx.x * ROWS + (int)threadIdx.x / L; row < a.N; row += (int64_t)gridDim.x * ROWS) {
             for (unsigned long long todo = a.pending[row]; todo != 0ull; todo &= todo - 1ull) {
                 const RestGradient rest(under(a.rest_coef[row], a.grad_out), a.rest_max[row], a.scale);

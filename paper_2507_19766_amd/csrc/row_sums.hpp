@@ -91,6 +91,13 @@ __device__ __forceinline__ float wave_max(float x)
                   larger(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
 }
 
+// Vectors that hold a row.  V + kPerVec - 1 would pass 32 bits at the largest V.
+template <class Tr>
+constexpr int vectors_of(int32_t V)
+{
+    return (V - 1) / Tr::kPerVec + 1;
+}
+
 // A vector of a row; behind the row's end, and where V ends inside a vector, the filler.
 template <class Tr>
 __device__ __forceinline__ u32x4 load_vector(const typename Tr::elem* rowp, int32_t V, int i)

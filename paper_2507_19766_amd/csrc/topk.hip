@@ -354,7 +354,7 @@ __device__ void select_and_write(const TopkArgs& a, const typename Tr::elem* row
     if (n_groups <= kGroupsPerWave) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         each_element<Tr>(a, rowp, groups, n_groups, lane, 64, collect);
-        if (wave == 0 && tail > 0) collect(lane < tail ? Tr::load1(rowp + behind + lane) : kEmpty, (uint32_t)(behind + lane));
+        if (wave == 0 && tail > 0) collect(lane < tail ? Tr::load1(rowp + behind + lane) : kEmpty, (uint32_t)behind + (uint32_t)lane);
     }
     const bool overflow = n_groups > kGroupsPerWave || n_elems > kElemsPerWave;
     if (lane == 0) sh.found[wave] = overflow ? kOverflow : n_elems;
@@ -514,8 +514,7 @@ __device__ __forceinline__ Token token_of(const TopkArgs& a, const typename Tr::
 template <class Tr, int NT>
 __device__ __forceinline__ void finish_row(const TopkArgs& a, const typename Tr::elem* rowp, int64_t row, const Row& st, const Token& token, Shared<NT>& sh)
 {
-    constexpr int E = Tr::kPerVec;
-    const int all = (a.V + E - 1) / E, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
+    const int all = vectors_of<Tr>(a.V), ngroups = (all + (1 << a.lg) - 1) >> a.lg;
     const bool ok = st.m > kFloor && st.S >= 0.5 && st.S < 1.0e30;       // neither NaN, +infinity nor everything masked
     if (threadIdx.x == 0) {
         const double ln_s = log64(st.S);
@@ -553,7 +552,7 @@ __global__ __launch_bounds__(NT, U == 4 && NT == 256 ? (Tr::kPerVec == 4 ? 8 : 7
     if (row >= a.N) return;
     const typename Tr::elem* rowp = logits + row * a.row_stride;
     const Token token = token_of<Tr>(a, rowp, row);
-    const Lane acc = stream_vectors<Tr, LG, U, NT>(a, rowp, 0, (a.V + Tr::kPerVec - 1) / Tr::kPerVec, sh);
+    const Lane acc = stream_vectors<Tr, LG, U, NT>(a, rowp, 0, vectors_of<Tr>(a.V), sh);
     const Row st = merge_lanes(acc, a.scale, sh);       // its barrier also closes the groups' maxima
     finish_row<Tr, NT>(a, rowp, row, st, token, sh);
 }
@@ -568,7 +567,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_piece_kernel(const typename
 {
     __shared__ Shared<kTopkThreads> sh;
     const int64_t row = blockIdx.y;
-    const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
+    const int all = vectors_of<Tr>(a.V);
     const int begin = (int)blockIdx.x * a.piece_vectors, end = min(all, begin + a.piece_vectors);
     const Lane acc = stream_vectors<Tr, LG, 4, kTopkThreads>(a, logits + row * a.row_stride, begin, end, sh);
     const Row st = merge_lanes(acc, a.scale, sh);
@@ -587,7 +586,7 @@ __global__ __launch_bounds__(kMergeThreads) void topk_merge_kernel(const typenam
     const typename Tr::elem* rowp = logits + row * a.row_stride;
     const RowParts& from = parts[row];
     const Token token = token_of<Tr>(a, rowp, row);
-    const int all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec, ngroups = (all + (1 << a.lg) - 1) >> a.lg;
+    const int all = vectors_of<Tr>(a.V), ngroups = (all + (1 << a.lg) - 1) >> a.lg;
 #pragma unroll
     for (int i = 0; i < groups_per_lane(kMergeThreads); ++i)
         if (i * kMergeThreads + tid < ngroups) sh.gmax[i * kMergeThreads + tid] = from.gmax[i * kMergeThreads + tid];
@@ -624,7 +623,7 @@ template <class Tr>
 void launch_topk(const void* logits, TopkArgs a, RowParts* parts, hipStream_t st)
 {
     const typename Tr::elem* z = (const typename Tr::elem*)logits;
-    const int64_t all = (a.V + Tr::kPerVec - 1) / Tr::kPerVec;
+    const int64_t all = vectors_of<Tr>(a.V);
     a.lg = 0;
     while (((all + ((int64_t)1 << a.lg) - 1) >> a.lg) > kMaxGroups) ++a.lg;
     // Pieces of whole batches of 1024 vectors, as many as bring the launch to about kFewWorkgroups workgroups.
