@@ -307,7 +307,8 @@ int32_t ulorl_token_loss_fwd_bwd_static(
  *                      token_ids may be NULL (logp is not written then and may be NULL)
  *   top_ids   [N, K]   int32, the K largest logits in falling order; of equal logits (+0 and -0 are) the lower id first
  *   top_logp  [N, K]   their x - lse
- * logits, N, V and row_stride as in ulorl_token_loss_fwd, N < 2^31; 1 <= K <= 128; temperature in [1e-3, 1e3].
+ * logits, N, V and row_stride as in ulorl_token_loss_fwd, N < 2^31, a lone row (N = 1) of any row_stride; 1 <= K <= 128;
+ * temperature in [1e-3, 1e3].
  * A logit at or below -9e29, -infinity included, is MASKED: it has probability 0 and is no alternative; where
  * fewer than K tokens are left (V < K too) the last ids are -1 and their log-probs -infinity.  A row that holds
  * not-a-number or +infinity, or nothing but masked logits, gets not-a-number everywhere and ids of -1.

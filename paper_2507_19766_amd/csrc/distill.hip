@@ -836,7 +836,7 @@ bool temperature_ok(float t) { return t >= 1.0e-3f && t <= 1.0e3f; }
 
 int32_t check_distill(const void* logits, int32_t dt, int64_t N, int64_t V, int64_t& row_stride, const int32_t* ids, int32_t K)
 {
-    if (N == 1 && row_stride >= V) row_stride = (V + 7) / 8 * 8;       // a lone row has no stride
+    row_stride = row_stride_of(N, V, row_stride);
     const int32_t rc = check_logits(logits, dt, N, V, row_stride);
     if (rc != ULORL_OK) return rc;
     if (N > kMaxDistillRows || K < 1 || K > kMaxK) return ULORL_ERR_SHAPE;

@@ -91,6 +91,12 @@ __device__ __forceinline__ float wave_max(float x)
                   larger(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
 }
 
+// The stride to check and to use: a lone row has none, whatever its caller's tensor says (a column taken as a row says 1).
+inline int64_t row_stride_of(int64_t N, int64_t V, int64_t row_stride)
+{
+    return N == 1 && V > 0 && V <= 0x7fffffffLL ? (V + 7) / 8 * 8 : row_stride;
+}
+
 // Vectors that hold a row.  V + kPerVec - 1 would pass 32 bits at the largest V.
 template <class Tr>
 constexpr int vectors_of(int32_t V)

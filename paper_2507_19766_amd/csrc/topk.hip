@@ -679,7 +679,7 @@ int32_t ulorl_token_topk(const void* logits, int32_t dt, int64_t N, int64_t V, i
                          int32_t K, float temperature, int32_t* top_ids, float* top_logp, float* logp, float* entropy, float* lse,
                          void* workspace, size_t workspace_bytes, void* hip_stream)
 {
-    if (N == 1 && row_stride >= V) row_stride = (V + 7) / 8 * 8;       // a lone row has no stride
+    row_stride = row_stride_of(N, V, row_stride);
     int32_t rc = check_logits(logits, dt, N, V, row_stride);
     if (rc != ULORL_OK) return rc;
     if (N > 0x7fffffffLL || K < 1 || K > kMaxK) return ULORL_ERR_SHAPE;
