@@ -301,8 +301,9 @@ TopFields token_topk(const Tensor& z, int64_t K, const OptTensor& token_ids, dou
     TopFields f;
     if (out.has_value()) {
         for (int i = 0; i < TOP_FIELDS; ++i) {
+            if (i == TOP_TOKEN_LOGP && !token_ids.has_value()) continue;        // not written, so not handed back either
             if ((*out)[i].has_value()) f[i] = *(*out)[i];
-            TORCH_CHECK_VALUE(f[i].defined() || (i == TOP_TOKEN_LOGP && !token_ids.has_value()), "out lacks a tensor");
+            TORCH_CHECK_VALUE(f[i].defined(), "out lacks a tensor");
         }
         check_matrix(f[TOP_IDS], at::kInt, l.N, K, "out.top_ids", l.dev);
         check_matrix(f[TOP_LOGP], at::kFloat, l.N, K, "out.top_logp", l.dev);
